@@ -389,6 +389,81 @@ msd_status_t msd_attn_decode_softmax_rule(int32_t B, int32_t Hq, int32_t Hkv, in
  * written for every token of the sequences, visible to the row or not.  NULL switches a dump off. */
 void msd_debug_set_attn_dump(int8_t* q_dbg, float* q_scale_dbg, int32_t* s_dbg);
 
+/*
+ * A PAGED key-value cache that is written, read and kept small by the three calls below (serving; the paper's kernels read a
+ * cache that is there, Alg. 3).  Token u of sequence b is row (block_table[b][u / page_size], u % page_size) of
+ *   k [num_blocks, page_size, Hkv, D], v [num_blocks, page_size, Hkv, Dv]: BF16, or INT8 codes with one FP32 scale per token and KV
+ *   head (k_scale, v_scale [num_blocks, page_size, Hkv]; value = scale * code), the layout that msd_attn_decode_int8kv_paged reads.
+ * The last dimension is contiguous; the others have strides in ELEMENTS {block, token, head}, so [num_blocks, Hkv, page_size, D] or
+ * k and v side by side in one allocation will do.  k, v 16-byte aligned, their strides multiples of 16 bytes, none negative;
+ * D, Dv multiples of 8 (BF16) or 16 (INT8), at most 256 (more: MSD_ERR_UNSUPPORTED); page_size 1 to 65536, any number.
+ * The struct is read during the call and lies in HOST memory.
+ *
+ * block_table [B, max_blocks] and seqlens [B] are INT32 on the device.  Entries of a row past ceil(length / page_size) are never read.
+ * A length below 0 or above what the call has room for, or an entry outside [0, num_blocks), is reported as MSD_ERR_BAD_SHAPE by
+ * msd_last_device_status; the results of that sequence are then unspecified, but nothing outside the buffers is touched.
+ * A page may be listed by several sequences (a shared prefix) where it is read only.
+ */
+typedef enum { MSD_CACHE_BF16 = 0, MSD_CACHE_INT8 = 1 } msd_cache_type_t;
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;                        /* INT8 only */
+  msd_cache_type_t type;
+  int64_t num_blocks;
+  int32_t page_size, Hkv, D, Dv;
+  int64_t k_stride[3], v_stride[3];                /* elements between blocks, tokens of a block, heads */
+  int64_t k_scale_stride[3], v_scale_stride[3];
+} msd_paged_cache_t;
+
+/*
+ * Puts new tokens into the cache.  seqlens: the lengths WITH the new tokens; sequence b has n_b = cu_new[b+1] - cu_new[b] of them
+ * (0 <= n_b <= seqlens[b]), rows cu_new[b] ... of k_new / v_new, and row cu_new[b] + i goes to position seqlens[b] - n_b + i.
+ *   k_new [n_rows, Hkv, D], v_new [n_rows, Hkv, Dv] BF16, 16-byte aligned, rows k_ld / v_ld elements apart (multiples of 8, so they may
+ *   be slices of a projection's result); cu_new [B+1] INT32 (device), not falling; rows from cu_new[B] on (padding) are left out.
+ * BF16 caches: copied.  INT8 caches, per row: scale = max|x| / 127, code = clamp(rne(x / scale), -127, 127), in IEEE FP32 with
+ * true divisions; a zero row gives scale 0 and codes 0.
+ *   weights nullable [B, Hkv, ld] FP32: the accumulated weights of msd_attn_decode_paged; those of the new positions are set to 0.
+ * No position may be written by two rows: a page that this call writes is listed by one sequence.
+ */
+msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16, int64_t n_rows, int64_t k_ld, int64_t v_ld,
+                                 const msd_paged_cache_t* cache, const int32_t* block_table, int32_t max_blocks, const int32_t* seqlens,
+                                 const int32_t* cu_new, int32_t B, float* weights, int64_t ld, void* stream);
+
+/*
+ * Attention of one new token per sequence over a paged cache, split over the cache's length and joined:
+ *   S_hj = softmax_scale * q_h . k_j,  P_h = softmax over the seqlens[b] tokens,  out_h = sum_j P_hj v_j,
+ * query head h reading KV head h / (Hq / Hkv).  Products of BF16 values (INT8 codes are exact in BF16; their scales are applied in FP32)
+ * with FP32 sums; softmax in FP32; P rounded to BF16 for the product with v.  No decomposition: this is the cache read as it is,
+ * beside msd_attn_decode_int8kv_paged, which splits q and P into INT8 components.
+ *   q_bf16 [B, Hq, D], rows of a sequence q_ld elements apart (a multiple of 8); out_bf16 [B, Hq, Dv]; lse nullable [B, Hq] FP32
+ *   (natural-log sum of exp of the scaled scores).  Hq % Hkv == 0.  Empty sequences give zeros and lse = -inf.
+ *   weights nullable [B, Hkv, ld] FP32: weights[b][k][j] += the sum of P_hj over the heads h of KV head k, for j < seqlens[b]; the
+ *   rest is left as it is.  ld >= every length.  The sums have a fixed order: equal inputs give equal bits.
+ * workspace: >= msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld) bytes (ld = 0 without weights), 1024-byte aligned, no
+ * initialisation needed.  Two kernels; nothing is kept from call to call.
+ */
+size_t msd_attn_decode_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Dv, int64_t ld);
+msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_paged_cache_t* cache, const int32_t* block_table,
+                                   int32_t max_blocks, const int32_t* seqlens, int32_t B, int32_t Hq, float softmax_scale, void* out_bf16,
+                                   float* lse, float* weights, int64_t ld, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight.  Per sequence b and KV head k, with L = seqlens[b]: L <= budget keeps every token; otherwise
+ * the first `sinks`, the last `recent`, and of the others the budget - sinks - recent with the largest weights[b][k][j] (of equal ones the
+ * lower j; NaN counts as the largest, -0 as 0).  Kept tokens stay in order; the i-th goes to position i of dst_block_table, so heads
+ * may keep different tokens (attention to one new token does not ask which).
+ *   new_seqlens [B] INT32 = min(L, budget); new_weights [B, Hkv, new_ld] FP32 and kept [B, Hkv, budget] INT32 (the j of each kept
+ *   token) are written up to there, the rest is left as it is.  0 <= sinks, recent; sinks + recent <= budget; 1 <= budget <= new_ld.
+ * The rows (and INT8 scales) are COPIED to the pages of dst_block_table [B, dst_max_blocks], which has room for min(L, budget) tokens
+ * of each sequence; the old pages are only read, so they may be shared with sequences outside the call, and are the caller's
+ * to hand out again afterwards.  A page of dst_block_table appears nowhere else in it and in no row of block_table; the same pointer
+ * for both is MSD_ERR_UNSUPPORTED, and so are new_weights == weights and new_seqlens == seqlens.
+ */
+msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* block_table, int32_t max_blocks, const int32_t* seqlens,
+                                const float* weights, int64_t ld, int32_t B, int32_t budget, int32_t recent, int32_t sinks,
+                                const int32_t* dst_block_table, int32_t dst_max_blocks, int32_t* new_seqlens, float* new_weights,
+                                int64_t new_ld, int32_t* kept, void* stream);
+
 /* Comparison kernel, not part of the MSD path: the cache expansion that MSD attention removes (Sec. 2.3; the
  * "Dequant" arm of Sec. 6.4).  out[t,h,:] = bf16(scale[t,h] * cache[t,h,:]), FP32 product rounded to nearest even.
  * cache [T,H,D] INT8, scale [T,H] FP32, out [T,H,D] BF16, all device pointers; cache and out 16-byte aligned;

@@ -76,6 +76,10 @@ _SIGS = {
     "msd_attn_decode_int8kv_spec": (C.c_int, [_vp] * 6 + [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _vp, _vp, _vp, _sz, _vp]),
     "msd_attn_decode_int8kv_paged": (C.c_int, [_vp] * 7 + [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _vp, _vp, _vp,
                                                 _sz, _vp]),
+    "msd_kv_append_paged": (C.c_int, [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp]),
+    "msd_attn_decode_paged_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _i64]),
+    "msd_attn_decode_paged": (C.c_int, [_vp, _i64, _vp, _vp, _i32, _vp, _i32, _i32, _f32, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "msd_kv_evict_paged": (C.c_int, [_vp, _vp, _i32, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp, _vp]),
     "msd_debug_timeout_selftest": (C.c_int, [_i64, _vp]),
     "msd_kv_dequant_bf16": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, _i32, _i32, C.c_void_p, C.c_void_p]),
     "msd_attn_decode_bf16kv_workspace_bytes": (_sz, [_i32] * 6),
@@ -468,6 +472,65 @@ def attn_decode_int8kv_paged(q, k, v, k_scale, v_scale, block_table, seqlens, pa
     if code != MSD_OK:
         raise MsdError(code, "msd_attn_decode_int8kv_paged")
     return (out, lse) if want_lse else out
+
+
+class PagedCache(C.Structure):
+    """msd_paged_cache_t, for calls of the C ABI through ctypes (the wrappers below take the tensors themselves)."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("type", C.c_int), ("num_blocks", _i64), ("page_size", _i32),
+                ("Hkv", _i32), ("D", _i32), ("Dv", _i32), ("k_stride", _i64 * 3), ("v_stride", _i64 * 3), ("k_scale_stride", _i64 * 3),
+                ("v_scale_stride", _i64 * 3)]
+
+
+def kv_append_paged(k_new, v_new, k, v, k_scale, v_scale, block_table, seqlens, cu_new, weights=None):
+    """New tokens go into a paged cache: k_new [n,Hkv,D], v_new [n,Hkv,Dv] bf16 (rows may be slices of a wider tensor), cache
+    k [blocks,page,Hkv,D], v [blocks,page,Hkv,Dv] bf16 with k_scale = v_scale = None, or int8 with scales [blocks,page,Hkv] f32 (any
+    strides, last dimension contiguous); block_table [B,max_blocks], seqlens [B] (with the new tokens), cu_new [B+1] int32.  Rows
+    cu_new[b] ... of sequence b become its last tokens.  weights [B,Hkv,ld] f32: those of the new positions are set to 0."""
+    code = _calls().kv_append_paged(k_new, v_new, k, v, k_scale, v_scale, block_table, seqlens, cu_new, weights)
+    if code != MSD_OK:
+        raise MsdError(code, "msd_kv_append_paged")
+
+
+def attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld=0):
+    """ld: positions that `weights` has room for (its last dimension), 0 without weights."""
+    return int(lib().msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld))
+
+
+def attn_decode_paged(q, k, v, k_scale, v_scale, block_table, seqlens, softmax_scale, weights=None, ws=None, want_lse=False, out=None):
+    """One new token of every sequence attends to its paged cache (as for kv_append_paged): q [B,Hq,D] bf16 -> out [B,Hq,Dv] bf16.
+    weights [B,Hkv,ld] f32: the attention weight of each cached token, summed over the heads of its KV head, is added to it."""
+    if ws is None or out is None or want_lse:
+        _need_cuda(block_table, seqlens)
+        B, Hq = q.shape[0], q.shape[1]
+        Hkv, Dv = k.shape[2], v.shape[3]
+        if ws is None:
+            ws = workspace(attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, 0 if weights is None else weights.shape[-1]), q.device)
+        if out is None:
+            out = _empty((B, Hq, Dv), torch.bfloat16, q.device)
+    lse = _empty((B, Hq), torch.float32, q.device) if want_lse else None
+    code = _calls().attn_decode_paged(q, k, v, k_scale, v_scale, block_table, seqlens, softmax_scale, weights, ws, out, lse)
+    if code != MSD_OK:
+        raise MsdError(code, "msd_attn_decode_paged")
+    return (out, lse) if want_lse else out
+
+
+def kv_evict_paged(k, v, k_scale, v_scale, block_table, seqlens, weights, budget, dst_block_table, recent=0, sinks=0, new_seqlens=None,
+                   new_weights=None, kept=None):
+    """Sequences longer than `budget` keep their first `sinks` tokens, their last `recent` ones and the others with the largest
+    accumulated weights [B,Hkv,ld] (per KV head; ties: the earlier token), in order; the kept rows are copied to the pages of
+    dst_block_table [B,dst_max_blocks] int32.  Returns (new_seqlens [B] int32, new_weights [B,Hkv,ld] f32, kept [B,Hkv,budget] int32);
+    of the last two only the first min(length, budget) entries of a row are written."""
+    if new_seqlens is None:
+        new_seqlens = _empty(seqlens.shape[0], torch.int32, seqlens.device)
+    if new_weights is None:
+        new_weights = _empty((weights.shape[0], weights.shape[1], max(weights.shape[2], int(budget))), torch.float32, weights.device).zero_()
+    if kept is None:
+        kept = _empty((weights.shape[0], weights.shape[1], int(budget)), torch.int32, weights.device).zero_()
+    code = _calls().kv_evict_paged(k, v, k_scale, v_scale, block_table, seqlens, weights, budget, recent, sinks, dst_block_table, new_seqlens,
+                                   new_weights, kept)
+    if code != MSD_OK:
+        raise MsdError(code, "msd_kv_evict_paged")
+    return new_seqlens, new_weights, kept
 
 
 def kv_dequant_bf16(cache, scale, out=None):

@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,6 +28,8 @@ class Args {
   bool ok() const { return ok_; }
 
   const at::Tensor* tensor(bool nullable = false) { return take(nullable, false); }
+  // a CUDA tensor of any strides (the caller of this looks at them)
+  const at::Tensor* strided(bool nullable = false) { return take(nullable, false, false); }
   // written by the kernels: a contiguous CUDA tensor, or page-locked host memory that they can reach
   const at::Tensor* buffer(bool nullable = false) { return take(nullable, true); }
   int64_t integer() {
@@ -49,7 +52,7 @@ class Args {
   }
 
  private:
-  const at::Tensor* take(bool nullable, bool pinned) {
+  const at::Tensor* take(bool nullable, bool pinned, bool contiguous = true) {
     PyObject* o = next();
     if (!o) return nullptr;
     if (o == Py_None && nullable) return nullptr;
@@ -58,8 +61,8 @@ class Args {
       return nullptr;
     }
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!(t.is_cuda() || (pinned && t.is_pinned())) || !t.is_contiguous()) {
-      fail(PyExc_ValueError, "expected contiguous CUDA tensors");
+    if (!(t.is_cuda() || (pinned && t.is_pinned())) || (contiguous && !t.is_contiguous())) {
+      fail(PyExc_ValueError, contiguous ? "expected contiguous CUDA tensors" : "expected CUDA tensors");
       return nullptr;
     }
     return &t;
@@ -271,6 +274,162 @@ PyObject* attn_decode_int8kv_paged(PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// ---- the paged cache that is written, read and shortened ----
+
+struct Typed {
+  const at::Tensor* t;
+  at::ScalarType type;
+  int rank;
+};
+// Types, ranks and device of a call's tensors (the ones that are there): all on the current device, whose stream the call goes to.
+bool typed(Args& a, std::initializer_list<Typed> want) {
+  if (!a.ok()) return false;
+  const auto device = c10::cuda::current_device();
+  for (const auto& w : want) {
+    if (!w.t) continue;
+    if (w.t->scalar_type() != w.type) a.fail(PyExc_TypeError, "a tensor has the wrong type");
+    else if (w.t->dim() != w.rank) a.fail(PyExc_ValueError, "a tensor has the wrong number of dimensions");
+    else if (w.t->get_device() != device) a.fail(PyExc_ValueError, "expected tensors on the current CUDA device");
+  }
+  return a.ok();
+}
+bool agree(Args& a, bool ok, const char* what) {
+  if (a.ok() && !ok) a.fail(PyExc_ValueError, what);
+  return a.ok();
+}
+
+// The last dimension of a tensor lies together.
+bool packed_rows(const at::Tensor* t) { return t->size(t->dim() - 1) == 1 || t->stride(t->dim() - 1) == 1; }
+
+// k, v [blocks, page, Hkv, D / Dv] and, for INT8, k_scale, v_scale [blocks, page, Hkv]
+bool paged_cache(Args& a, const at::Tensor* k, const at::Tensor* v, const at::Tensor* ks, const at::Tensor* vs, msd_paged_cache_t* c) {
+  if (!a.ok()) return false;
+  const auto type = k->scalar_type();
+  if (type != at::kBFloat16 && type != at::kChar) {
+    a.fail(PyExc_TypeError, "expected a cache of bfloat16 or int8");
+    return false;
+  }
+  const bool int8 = type == at::kChar;
+  if (!typed(a, {{k, type, 4}, {v, type, 4}, {ks, at::kFloat, 3}, {vs, at::kFloat, 3}})) return false;
+  if (!agree(a, int8 ? ks && vs : !ks && !vs, "scales go with an int8 cache, both of them, and with no other")) return false;
+  if (!agree(a, packed_rows(k) && packed_rows(v), "the last dimension of k and v has to be contiguous")) return false;
+  for (int i = 0; i < 3; ++i)
+    if (!agree(a, v->size(i) == k->size(i) && (!ks || (ks->size(i) == k->size(i) && vs->size(i) == k->size(i))), "the parts of a cache differ in their sizes"))
+      return false;
+  if (!agree(a, k->size(1) <= 0x7FFFFFFF && k->size(2) <= 0x7FFFFFFF && k->size(3) <= 0x7FFFFFFF && v->size(3) <= 0x7FFFFFFF, "a size is too large")) return false;
+  *c = msd_paged_cache_t{};
+  c->k = k->data_ptr();
+  c->v = v->data_ptr();
+  c->k_scale = addr_as<float>(ks);
+  c->v_scale = addr_as<float>(vs);
+  c->type = int8 ? MSD_CACHE_INT8 : MSD_CACHE_BF16;
+  c->num_blocks = k->size(0);
+  c->page_size = static_cast<int32_t>(k->size(1));
+  c->Hkv = static_cast<int32_t>(k->size(2));
+  c->D = static_cast<int32_t>(k->size(3));
+  c->Dv = static_cast<int32_t>(v->size(3));
+  for (int i = 0; i < 3; ++i) {      // (a dimension of one has no stride that matters)
+    const bool one = k->size(i) == 1;
+    c->k_stride[i] = one ? 0 : k->stride(i);
+    c->v_stride[i] = one ? 0 : v->stride(i);
+    if (int8) {
+      c->k_scale_stride[i] = one ? 0 : ks->stride(i);
+      c->v_scale_stride[i] = one ? 0 : vs->stride(i);
+    }
+  }
+  return true;
+}
+
+// [n, heads, D]: rows of `heads` heads lie together, row after row with any stride
+bool head_rows(const at::Tensor* t) {
+  return t->dim() == 3 && packed_rows(t) && (t->size(1) == 1 || t->stride(1) == t->size(2));
+}
+int64_t row_stride(const at::Tensor* t) { return t->size(0) <= 1 ? t->size(1) * t->size(2) : t->stride(0); }
+
+// (k_new, v_new, k, v, k_scale or None, v_scale or None, block_table, seqlens, cu_new, weights or None)
+PyObject* kv_append_paged(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n);
+  const at::Tensor *kn = a.strided(), *vn = a.strided(), *k = a.strided(), *v = a.strided(), *ks = a.strided(true), *vs = a.strided(true),
+                   *table = a.tensor(), *len = a.tensor(), *cu = a.tensor(), *w = a.tensor(true);
+  msd_paged_cache_t c;
+  if (!paged_cache(a, k, v, ks, vs, &c) ||
+      !typed(a, {{kn, at::kBFloat16, 3}, {vn, at::kBFloat16, 3}, {table, at::kInt, 2}, {len, at::kInt, 1}, {cu, at::kInt, 1}, {w, at::kFloat, 3}}) ||
+      !agree(a, head_rows(kn) && head_rows(vn), "a row of k_new or v_new has to be contiguous") ||
+      !agree(a, kn->size(0) == vn->size(0) && kn->size(1) == c.Hkv && vn->size(1) == c.Hkv && kn->size(2) == c.D && vn->size(2) == c.Dv,
+             "k_new and v_new do not fit the cache") ||
+      !agree(a, table->size(0) == len->size(0) && cu->size(0) == len->size(0) + 1, "block_table, seqlens and cu_new differ in their sequences") ||
+      !agree(a, len->size(0) <= 0x7FFFFFFF && table->size(1) <= 0x7FFFFFFF, "a size is too large") ||
+      !agree(a, !w || (w->size(0) == len->size(0) && w->size(1) == c.Hkv), "weights: [sequences, KV heads, positions]"))
+    return nullptr;
+  void *knp = addr(kn), *vnp = addr(vn), *st = stream();
+  const int64_t rows = kn->size(0), k_ld = row_stride(kn), v_ld = row_stride(vn), ld = w ? w->size(2) : 0;
+  const int32_t B = static_cast<int32_t>(len->size(0)), blocks = static_cast<int32_t>(table->size(1));
+  const auto *tp = addr_as<int32_t>(table), *lp = addr_as<int32_t>(len), *cp = addr_as<int32_t>(cu);
+  auto* wp = addr_as<float>(w);
+  return status_of([&] { return msd_kv_append_paged(knp, vnp, rows, k_ld, v_ld, &c, tp, blocks, lp, cp, B, wp, ld, st); });
+}
+
+// (q, k, v, k_scale or None, v_scale or None, block_table, seqlens, softmax_scale, weights or None, ws, out, lse or None)
+PyObject* attn_decode_paged(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n);
+  const at::Tensor *q = a.strided(), *k = a.strided(), *v = a.strided(), *ks = a.strided(true), *vs = a.strided(true), *table = a.tensor(),
+                   *len = a.tensor();
+  const float scale = static_cast<float>(a.number());
+  const at::Tensor *w = a.tensor(true), *ws = a.tensor(), *out = a.tensor(), *lse = a.tensor(true);
+  msd_paged_cache_t c;
+  if (!paged_cache(a, k, v, ks, vs, &c) ||
+      !typed(a, {{q, at::kBFloat16, 3}, {table, at::kInt, 2}, {len, at::kInt, 1}, {w, at::kFloat, 3}, {out, at::kBFloat16, 3}, {lse, at::kFloat, 2},
+                 {ws, ws ? ws->scalar_type() : at::kByte, ws ? static_cast<int>(ws->dim()) : 1}}) ||
+      !agree(a, head_rows(q), "a sequence's rows of q have to be contiguous") || !agree(a, q->size(2) == c.D, "q and k differ in the size of a head") ||
+      !agree(a, table->size(0) == q->size(0) && len->size(0) == q->size(0), "q, block_table and seqlens differ in their sequences") ||
+      !agree(a, q->size(0) <= 0x7FFFFFFF && q->size(1) <= 0x7FFFFFFF && table->size(1) <= 0x7FFFFFFF, "a size is too large") ||
+      !agree(a, out->size(0) == q->size(0) && out->size(1) == q->size(1) && out->size(2) == c.Dv, "out: [sequences, heads, size of a value]") ||
+      !agree(a, !lse || (lse->size(0) == q->size(0) && lse->size(1) == q->size(1)), "lse: [sequences, heads]") ||
+      !agree(a, !w || (w->size(0) == q->size(0) && w->size(1) == c.Hkv), "weights: [sequences, KV heads, positions]"))
+    return nullptr;
+  const Workspace room(ws);
+  void *qp = addr(q), *op = addr(out), *st = stream();
+  const int64_t q_ld = row_stride(q), ld = w ? w->size(2) : 0;
+  const int32_t B = static_cast<int32_t>(q->size(0)), Hq = static_cast<int32_t>(q->size(1)), blocks = static_cast<int32_t>(table->size(1));
+  const auto *tp = addr_as<int32_t>(table), *np = addr_as<int32_t>(len);
+  auto *wp = addr_as<float>(w), *lp = addr_as<float>(lse);
+  return status_of([&] { return msd_attn_decode_paged(qp, q_ld, &c, tp, blocks, np, B, Hq, scale, op, lp, wp, ld, room.p, room.bytes, st); });
+}
+
+// (k, v, k_scale or None, v_scale or None, block_table, seqlens, weights, budget, recent, sinks, dst_block_table, new_seqlens, new_weights, kept)
+PyObject* kv_evict_paged(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n);
+  const at::Tensor *k = a.strided(), *v = a.strided(), *ks = a.strided(true), *vs = a.strided(true), *table = a.tensor(), *len = a.tensor(),
+                   *w = a.tensor();
+  const int64_t budget = a.integer(), recent = a.integer(), sinks = a.integer();
+  const at::Tensor *to = a.tensor(), *new_len = a.tensor(), *new_w = a.tensor(), *kept = a.tensor();
+  msd_paged_cache_t c;
+  if (!paged_cache(a, k, v, ks, vs, &c) ||
+      !typed(a, {{table, at::kInt, 2}, {len, at::kInt, 1}, {w, at::kFloat, 3}, {to, at::kInt, 2}, {new_len, at::kInt, 1}, {new_w, at::kFloat, 3},
+                 {kept, at::kInt, 3}}))
+    return nullptr;
+  const int64_t B = len->size(0);
+  if (!agree(a, B <= 0x7FFFFFFF && table->size(1) <= 0x7FFFFFFF && to->size(1) <= 0x7FFFFFFF, "a size is too large") ||
+      !agree(a, budget >= 1 && budget <= 0x7FFFFFFF && recent >= 0 && sinks >= 0 && recent <= budget && sinks <= budget,
+             "budget is at least 1, and recent and sinks are from 0 to budget") ||
+      !agree(a, table->size(0) == B && to->size(0) == B && new_len->size(0) == B && w->size(0) == B && new_w->size(0) == B && kept->size(0) == B,
+             "the tensors differ in their sequences") ||
+      !agree(a, w->size(1) == c.Hkv && new_w->size(1) == c.Hkv && kept->size(1) == c.Hkv, "the tensors differ in their KV heads") ||
+      !agree(a, kept->size(2) == budget, "kept: [sequences, KV heads, budget]"))
+    return nullptr;
+  const int64_t ld = w->size(2), new_ld = new_w->size(2);
+  const int32_t blocks = static_cast<int32_t>(table->size(1)), to_blocks = static_cast<int32_t>(to->size(1));
+  const auto *tp = addr_as<int32_t>(table), *lp = addr_as<int32_t>(len), *dp = addr_as<int32_t>(to);
+  const auto* wp = addr_as<float>(w);
+  auto *nlp = addr_as<int32_t>(new_len), *kp = addr_as<int32_t>(kept);
+  auto* nwp = addr_as<float>(new_w);
+  void* st = stream();
+  return status_of([&] {
+    return msd_kv_evict_paged(&c, tp, blocks, lp, wp, ld, static_cast<int32_t>(B), static_cast<int32_t>(budget), static_cast<int32_t>(recent),
+                              static_cast<int32_t>(sinks), dp, to_blocks, nlp, nwp, new_ld, kp, st);
+  });
+}
+
 // What the interpreter calls: C++ exceptions (a tensor without storage or with another layout, no memory) become Python's.
 template <PyObject* (*fn)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -288,6 +447,7 @@ PyMethodDef methods[] = {
     method<gemm_w8a16>("gemm_w8a16"), method<gemm_w4a16>("gemm_w4a16"), method<grouped_gemm_w8a16>("grouped_gemm_w8a16"),
     method<grouped_gemm_w4a16>("grouped_gemm_w4a16"), method<attn_decode<false>>("attn_decode_int8kv"),
     method<attn_decode<true>>("attn_decode_int8kv_spec"), method<attn_decode_int8kv_paged>("attn_decode_int8kv_paged"),
+    method<kv_append_paged>("kv_append_paged"), method<attn_decode_paged>("attn_decode_paged"), method<kv_evict_paged>("kv_evict_paged"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

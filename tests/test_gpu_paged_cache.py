@@ -1,0 +1,497 @@
+"""The paged cache on the GPU: appending, attention of one new token with the weights of the cached tokens, eviction; each against
+plain 64-bit loops, at the sizes and masks where it can go wrong, and all of them as a decoding loop runs them."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_13915_b200 import binding, inputs
+from paged_reference import attention, evicted, make_cache
+
+pytestmark = pytest.mark.gpu
+
+HALF_BF16 = torch.finfo(torch.bfloat16).eps / 2      # 2^-8: one rounding to BF16
+FP32 = 2.0 ** -23                                     # one FP32 operation, rounded or cut
+
+
+def _args(c):
+    return c["k"], c["v"], c["k_scale"], c["v_scale"], c["table"], c["seqlens"]
+
+
+def _check_attention(q, c, scale, got, lse=None, before=None, weights=None):
+    """What the arithmetic allows: a score is a sum of D products in FP32, then scaled (and for INT8 scaled again): off by at most
+    d = (D + 8) 2^-23 sum |q k| scale; the softmax of scores that are off by d has probabilities off by a factor e^(2d), and exp2, the
+    sums and the division add a few FP32 roundings (16 are granted).  P (INT8: times the value's scale) is rounded to BF16 once,
+    the result once more."""
+    want, want_lse, want_w, mass, reach = attention(q, c, scale)
+    D = q.shape[2]
+    d = (D + 8) * FP32 * reach
+    rel = torch.expm1(2 * d) + 16 * FP32
+    # sums over the tokens: FP32 additions in chains of at most (length / 64 + 64)
+    longest = int(c["seqlens"].max()) if len(c["seqlens"]) else 0
+    rel = rel + (longest / 64 + 64) * FP32
+    bound = HALF_BF16 * want.abs() + (HALF_BF16 + rel[..., None]) * mass * (1 + 2 * HALF_BF16)
+    assert torch.isfinite(got.float()).all()
+    assert ((got.double() - want).abs() <= bound + 1e-38).all(), ((got.double() - want).abs() - bound).max()
+    if lse is not None:
+        empty = want_lse == float("-inf")
+        assert torch.equal(lse == float("-inf"), empty)
+        diff = torch.where(empty, 0.0, (lse.double() - torch.where(empty, 0.0, want_lse)).abs())
+        assert (diff <= d + rel + 4 * FP32 * torch.where(empty, 0.0, want_lse.abs())).all()
+    if weights is not None:
+        G = q.shape[1] // c["k"].shape[2]
+        for b, w in enumerate(want_w):
+            n = w.shape[1]
+            assert torch.equal(weights[b, :, n:], before[b, :, n:]), "weights past the last token were touched"
+            r = rel[b].view(-1, G).amax(-1)[:, None] if n else 0.0
+            total = before[b, :, :n].double() + w
+            assert ((weights[b, :, :n].double() - total).abs() <= w * (r + G * FP32) + total * FP32 + 1e-38).all()
+
+
+# (lengths, Hq, Hkv, D, Dv, page, layout): a tile is 64 or 128 tokens
+SHAPES = [
+    ([1], 4, 1, 64, 64, 16, "tokens"),
+    ([0], 4, 1, 128, 128, 16, "tokens"),
+    ([5, 0, 64, 63, 65, 0, 127, 128, 129, 1], 8, 2, 128, 128, 16, "tokens"),
+    ([300, 17, 1000], 12, 12, 64, 64, 8, "heads"),
+    ([700, 33], 32, 4, 128, 128, 64, "joint"),
+    ([257, 600], 32, 2, 128, 128, 20, "heads"),             # 16 query heads to a KV head, pages of 20
+    ([450, 31], 40, 2, 96, 96, 1, "tokens"),                # 20: a second group of heads; a page a token
+    ([513, 90], 7, 1, 80, 64, 32, "tokens"),
+    ([200, 1030], 10, 2, 64, 128, 128, "joint"),
+    ([333, 64], 8, 1, 256, 256, 16, "heads"),
+    ([129, 500], 6, 3, 192, 240, 48, "tokens"),
+    ([77], 17, 1, 16, 16, 16, "tokens"),
+    ([9000, 3, 0, 2500], 16, 4, 128, 128, 64, "tokens"),    # cut over many CTAs
+    ([20000], 8, 1, 64, 64, 100, "tokens"),
+]
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lengths,Hq,Hkv,D,Dv,page,layout", SHAPES)
+def test_attention(lengths, Hq, Hkv, D, Dv, page, layout, int8):
+    c = make_cache(lengths, Hkv, D, Dv, page, int8, seed=len(lengths) + D, layout=layout)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.randn(len(lengths), Hq, D, generator=g, device="cuda").to(torch.bfloat16)
+    before = torch.rand(len(lengths), Hkv, max(lengths) + 3, generator=g, device="cuda")
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+    # without weights the result is the same, bit for bit
+    assert torch.equal(binding.attn_decode_paged(q, *_args(c), D ** -0.5), out)
+    binding.last_device_status()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_of_many_short_sequences(int8):
+    """More sequences than the threads that cut the list of tiles, empty ones among them."""
+    g = torch.Generator().manual_seed(1)
+    lengths = torch.randint(0, 90, (700,), generator=g).tolist()
+    lengths[3] = lengths[698] = lengths[699] = 0
+    c = make_cache(lengths, 2, 64, 64, 16, int8, seed=4)
+    q = torch.randn(700, 4, 64, generator=g).to(torch.bfloat16).cuda()
+    before = torch.rand(700, 2, 90, generator=g).cuda()
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), 0.125, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, 0.125, out, lse, before, weights)
+
+
+def test_attention_of_nothing_but_empty_sequences():
+    c = make_cache([0, 0, 0], 2, 128, 128, 16)
+    q = torch.ones(3, 8, 128, dtype=torch.bfloat16, device="cuda")
+    weights = torch.full((3, 2, 7), 0.5, device="cuda")
+    out, lse = binding.attn_decode_paged(q, *_args(c), 0.1, weights=weights, want_lse=True)
+    binding.last_device_status()
+    assert (out == 0).all() and (lse == float("-inf")).all() and (weights == 0.5).all()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_with_scores_far_apart(int8):
+    """Scores of hundreds: the running maximum moves and most probabilities vanish."""
+    c = make_cache([900, 140], 2, 128, 128, 16, int8, seed=9, scale_of_k=30.0)
+    q = torch.randn(2, 8, 128, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    before = torch.zeros(2, 2, 900, device="cuda")
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), 1.0, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, 1.0, out, lse, before, weights)
+
+
+def test_attention_takes_slices_of_a_projection():
+    """q as a slice of a fused projection's result, on another stream than the default one."""
+    c = make_cache([130, 40], 2, 64, 64, 16, seed=3)
+    qkv = torch.randn(2, 8 + 4, 64, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    q = qkv[:, :8]
+    want = binding.attn_decode_paged(q.contiguous(), *_args(c), 0.125)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = binding.attn_decode_paged(q, *_args(c), 0.125)
+    s.synchronize()
+    assert torch.equal(got, want)
+    _check_attention(q, c, 0.125, got)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_gives_equal_bits_and_replays(int8):
+    """Equal inputs give equal bits, captured or not; a workspace full of rubbish does no harm; lengths may change between replays."""
+    c = make_cache([5000, 700, 64], 4, 128, 128, 16, int8, seed=6)
+    q = torch.randn(3, 16, 128, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16).cuda()
+    weights = torch.zeros(3, 4, 5000, device="cuda")
+    ws = binding.workspace(binding.attn_decode_paged_workspace_bytes(3, 16, 4, 128, 5000))
+    ws.fill_(0xFF)
+    out = torch.empty(3, 16, 128, dtype=torch.bfloat16, device="cuda")
+    call = lambda: binding.attn_decode_paged(q, *_args(c), 0.1, weights=weights, ws=ws, out=out)
+    call()
+    want, want_w = out.clone(), weights.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        call()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    torch.cuda.synchronize()
+    for _ in range(2):
+        weights.zero_()
+        out.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(weights, want_w)
+    c["seqlens"].copy_(torch.tensor([17, 0, 40], dtype=torch.int32))
+    weights.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    binding.last_device_status()
+    _check_attention(q, c, 0.1, out, None, torch.zeros_like(weights), weights)
+
+
+def test_attention_reports_pages_and_lengths_that_do_not_exist():
+    c = make_cache([100, 100], 1, 64, 64, 16, seed=2)
+    q = torch.ones(2, 2, 64, dtype=torch.bfloat16, device="cuda")
+    want = binding.attn_decode_paged(q, *_args(c), 0.1)
+    binding.last_device_status()
+    for bad in (-1, c["k"].shape[0], 2 ** 31 - 1):
+        t = c["table"].clone()
+        t[0, 2] = bad
+        got = binding.attn_decode_paged(q, c["k"], c["v"], None, None, t, c["seqlens"], 0.1)
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            binding.last_device_status()
+        assert torch.equal(got[1], want[1])
+    for bad in (-5, 113):
+        got = binding.attn_decode_paged(q, c["k"], c["v"], None, None, c["table"], torch.tensor([bad, 100], dtype=torch.int32, device="cuda"), 0.1)
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            binding.last_device_status()
+        assert torch.equal(got[1], want[1])
+    # weights with room for fewer positions than a sequence has
+    weights = torch.zeros(2, 1, 50, device="cuda")
+    binding.attn_decode_paged(q, *_args(c), 0.1, weights=weights)
+    with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+        binding.last_device_status()
+
+
+def test_attention_past_32_bit_offsets():
+    """A cache of more than 4 GB whose last pages are in use."""
+    page, Hkv, D = 64, 8, 128
+    blocks = (5 << 30) // (page * Hkv * D * 2)
+    small = make_cache([300, 150], Hkv, D, D, page, seed=8, spare=0)
+    k = torch.zeros(blocks, page, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    n = small["k"].shape[0]
+    k[-n:], v[-n:] = small["k"], small["v"]
+    table = torch.where(small["table"] >= 0, small["table"] + (blocks - n), -1).int()
+    q = torch.randn(2, 16, D, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).cuda()
+    got = binding.attn_decode_paged(q, k, v, None, None, table, small["seqlens"], 0.1)
+    binding.last_device_status()
+    assert torch.equal(got, binding.attn_decode_paged(q, *_args(small), 0.1))
+    _check_attention(q, small, 0.1, got)
+
+
+# ---- append ----------------------------------------------------------------------------------------------------------------
+def _append_reference(c, k_new, v_new, cu):
+    """The cache after the append, on the host; INT8 codes by the numpy quantizer that the tests of the other kernels use."""
+    k, v = c["k"].cpu().clone(), c["v"].cpu().clone()
+    ks, vs = (None, None) if c["k_scale"] is None else (c["k_scale"].cpu().clone(), c["v_scale"].cpu().clone())
+    table, lengths, page = c["table"].cpu(), c["seqlens"].tolist(), c["k"].shape[1]
+    for b, n in enumerate(lengths):
+        m = cu[b + 1] - cu[b]
+        for i in range(m):
+            pos = n - m + i
+            blk, slot = int(table[b, pos // page]), pos % page
+            for pool, scale, new in ((k, ks, k_new), (v, vs, v_new)):
+                row = new[cu[b] + i].cpu()
+                if scale is None:
+                    pool[blk, slot] = row
+                else:
+                    codes, s = inputs.quantize_rows_int8(row.contiguous().view(torch.int16).numpy().view(np.uint16))
+                    pool[blk, slot], scale[blk, slot] = torch.from_numpy(codes), torch.from_numpy(s)
+    return k, v, ks, vs
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lengths,new,Hkv,D,Dv,page,layout", [
+    ([1], [1], 1, 64, 64, 16, "tokens"),
+    ([40, 0, 7, 129], [1, 0, 7, 30], 8, 128, 128, 16, "tokens"),
+    ([300, 20], [300, 0], 3, 80, 96, 20, "heads"),
+    ([65, 64, 63], [65, 1, 2], 5, 256, 144, 1, "joint"),
+    ([33] * 70, [1] * 70, 2, 128, 64, 32, "tokens"),
+])
+def test_append(lengths, new, Hkv, D, Dv, page, layout, int8):
+    c = make_cache(lengths, Hkv, D, Dv, page, int8, seed=D, layout=layout, poison=False)
+    cu = [0]
+    for n in new:
+        cu.append(cu[-1] + n)
+    g = torch.Generator().manual_seed(7)
+    pad = 3                                               # rows behind the last sequence's, as in a padded batch
+    kv = torch.randn(cu[-1] + pad, Hkv * (D + Dv), generator=g).to(torch.bfloat16)
+    # short integers times a power of two: quotients that lie on or near a half; and rows of zeros, tiny and huge values
+    kv[:: 2] = (torch.randint(-127, 128, kv[::2].shape, generator=g).float() * 0.5).to(torch.bfloat16)
+    kv[0, :D] = 0
+    kv[-pad - 1] *= 2.0 ** -120
+    kv[cu[-1] // 2] *= 2.0 ** 118
+    kv = kv.cuda()
+    k_new, v_new = kv[:, :Hkv * D].unflatten(1, (Hkv, D)), kv[:, Hkv * D:].unflatten(1, (Hkv, Dv))      # slices: rows with a stride
+    weights = torch.full((len(lengths), Hkv, max(lengths) + 2), 0.25, device="cuda")
+    want = _append_reference(c, k_new, v_new, cu)
+    binding.kv_append_paged(k_new, v_new, *_args(c), torch.tensor(cu, dtype=torch.int32, device="cuda"), weights=weights)
+    binding.last_device_status()
+    for got, ref in zip((c["k"], c["v"], c["k_scale"], c["v_scale"]), want):
+        if ref is not None:
+            bits = {1: torch.int8, 2: torch.int16, 4: torch.int32}[ref.element_size()]
+            assert torch.equal(got.cpu().contiguous().view(bits), ref.contiguous().view(bits))
+    for b, n in enumerate(lengths):
+        m = new[b]
+        assert (weights[b, :, n - m:n] == 0).all() and (weights[b, :, :n - m] == 0.25).all() and (weights[b, :, n:] == 0.25).all()
+
+
+def test_append_reports_what_does_not_fit():
+    c = make_cache([20, 20], 2, 64, 64, 16, seed=1, poison=False)
+    new = torch.ones(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cu = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    before = c["k"].clone()
+
+    def reported(table, lengths, cu=cu):
+        binding.kv_append_paged(new, new, c["k"], c["v"], None, None, table, lengths, cu)
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            binding.last_device_status()
+
+    off = torch.full_like(c["table"], -1)
+    reported(off, c["seqlens"])
+    reported(torch.full_like(off, c["k"].shape[0]), c["seqlens"])
+    reported(c["table"], torch.tensor([33, 400], dtype=torch.int32, device="cuda"))       # no room in the table
+    reported(c["table"], torch.tensor([1, -3], dtype=torch.int32, device="cuda"))         # more new tokens than tokens
+    assert torch.equal(c["k"], before)
+
+
+# ---- eviction ----------------------------------------------------------------------------------------------------------------
+def _evict_case(lengths, Hkv, D, Dv, page, budget, int8, seed, layout="tokens"):
+    """A cache with pages left for what is kept; the destination pages are in random order too."""
+    kept = [min(n, budget) for n in lengths]
+    need = [(n + page - 1) // page for n in kept]
+    c = make_cache(lengths, Hkv, D, Dv, page, int8, seed=seed, layout=layout, spare=sum(need) + 2)
+    blocks = c["k"].shape[0]
+    used = set(c["table"][c["table"] >= 0].tolist())
+    free = [p for p in range(blocks) if p not in used]
+    g = torch.Generator().manual_seed(seed + 1)
+    free = [free[i] for i in torch.randperm(len(free), generator=g).tolist()]
+    dst = torch.full((len(lengths), max([1] + need)), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        for j in range(n):
+            dst[b, j] = free.pop()
+    return c, dst.cuda()
+
+
+def _check_evicted(c, dst, weights, got, budget, recent, sinks, pools):
+    new_seqlens, new_weights, kept = (t.cpu() for t in got)
+    table, to, w = c["table"].cpu(), dst.cpu(), weights.cpu()
+    page = c["k"].shape[1]
+    for b, n in enumerate(c["seqlens"].tolist()):
+        m = min(n, budget)
+        assert int(new_seqlens[b]) == m
+        for h in range(c["k"].shape[2]):
+            stay = evicted(w[b, h].tolist(), n, budget, recent, sinks)
+            assert kept[b, h, :m].tolist() == stay
+            if not m:
+                continue
+            src, at = torch.tensor(stay), torch.arange(m)
+            assert torch.equal(new_weights[b, h, :m].view(torch.int32), w[b, h, src].view(torch.int32))
+            for pool, before in pools:
+                if pool is None:
+                    continue
+                a = pool.cpu()[to[b, at // page].long(), at % page, h]
+                r = before[table[b, src // page].long(), src % page, h]
+                bits = {1: torch.int8, 2: torch.int16, 4: torch.int32}[a.element_size()]
+                assert torch.equal(a.contiguous().view(bits), r.contiguous().view(bits))
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lengths,Hkv,D,Dv,page,budget,recent,sinks,layout", [
+    ([1, 0, 5], 1, 64, 64, 16, 3, 1, 1, "tokens"),
+    ([700, 90, 512, 0, 64], 4, 128, 128, 16, 64, 10, 4, "tokens"),
+    ([300, 1000], 2, 80, 96, 20, 257, 0, 0, "heads"),
+    ([3000, 2100], 2, 128, 64, 64, 2048, 0, 2048, "tokens"),     # nothing but the first ones
+    ([777], 3, 256, 144, 32, 500, 500, 0, "joint"),               # nothing but the last ones
+    ([40], 1, 16, 16, 1, 1, 0, 0, "tokens"),
+    ([100, 100], 2, 64, 64, 16, 5000, 3, 3, "tokens"),            # room for everything
+])
+def test_eviction(lengths, Hkv, D, Dv, page, budget, recent, sinks, layout, int8):
+    c, dst = _evict_case(lengths, Hkv, D, Dv, page, budget, int8, seed=D + budget, layout=layout)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    weights = torch.rand(len(lengths), Hkv, max(lengths) + 1, generator=g, device="cuda").mul_(8).round_().div_(8)      # ties
+    pools = [(c[x], None if c[x] is None else c[x].cpu().clone()) for x in ("k", "v", "k_scale", "v_scale")]
+    got = binding.kv_evict_paged(*_args(c), weights, budget, dst, recent=recent, sinks=sinks)
+    binding.last_device_status()
+    _check_evicted(c, dst, weights, got, budget, recent, sinks, pools)
+    # nothing but the destination rows was written
+    written = torch.zeros(c["k"].shape[:2], dtype=torch.bool)
+    for b, n in enumerate(lengths):
+        at = torch.arange(min(n, budget))
+        written[dst.cpu()[b, at // page].long(), at % page] = True
+    for pool, before in pools:
+        if pool is not None:
+            bits = {1: torch.int8, 2: torch.int16, 4: torch.int32}[pool.element_size()]
+            assert torch.equal(pool.cpu()[~written].contiguous().view(bits), before[~written].contiguous().view(bits))
+
+
+@pytest.mark.parametrize("values", ["equal", "negative", "infinite", "nan", "tiny", "zeros"])
+def test_eviction_orders_every_kind_of_weight(values):
+    n, budget = 1500, 700
+    c, dst = _evict_case([n, n - 1], 2, 16, 16, 16, budget, True, seed=4)
+    w = torch.randn(2, 2, n, generator=torch.Generator().manual_seed(4))
+    w = {"equal": torch.full_like(w, 0.75), "negative": -w.abs(), "infinite": torch.where(w > 1, float("inf"), torch.where(w < -1, float("-inf"), w)),
+         "nan": torch.where(w > 0.2, float("nan"), w), "tiny": w * 1e-40, "zeros": torch.where(w > 0, 0.0, -0.0)}[values].cuda()
+    pools = [(c[x], c[x].cpu().clone()) for x in ("k", "v", "k_scale", "v_scale")]
+    got = binding.kv_evict_paged(*_args(c), w, budget, dst, recent=100, sinks=7)
+    binding.last_device_status()
+    _check_evicted(c, dst, w, got, budget, 100, 7, pools)
+
+
+@pytest.mark.parametrize("n,room", [(2048, 2048), (2049, 2049), (9000, 9000), (16385, 16385), (70000, 70000), (140000, 140000), (3000, 140000)])
+def test_eviction_of_long_sequences(n, room):
+    """Rows that a CTA holds, rows for clusters of two to eight, and rows that are read again in every round; and a short sequence
+    whose buffers have room for a long one."""
+    budget = n // 3
+    c, dst = _evict_case([n], 1, 16, 16, 64, budget, True, seed=5)
+    w = torch.randn(1, 1, room, generator=torch.Generator().manual_seed(5)).mul_(3).exp_()
+    w[..., ::3] = 1.0
+    w = w.cuda()
+    table = torch.full((1, (room + 63) // 64), -1, dtype=torch.int32, device="cuda")
+    table[:, :c["table"].shape[1]] = c["table"]
+    pools = [(c[x], c[x].cpu().clone()) for x in ("k", "v", "k_scale", "v_scale")]
+    got = binding.kv_evict_paged(c["k"], c["v"], c["k_scale"], c["v_scale"], table, c["seqlens"], w, budget, dst, recent=50, sinks=4)
+    binding.last_device_status()
+    _check_evicted(c, dst, w, got, budget, 50, 4, pools)
+
+
+def test_eviction_reports_what_does_not_fit():
+    c, dst = _evict_case([100, 100], 1, 64, 64, 16, 40, False, seed=2)
+    w = torch.rand(2, 1, 100, device="cuda")
+
+    def reported(table, lengths, to, weights=w):
+        binding.kv_evict_paged(c["k"], c["v"], None, None, table, lengths, weights, 40, to)
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            binding.last_device_status()
+
+    reported(torch.full_like(c["table"], -1), c["seqlens"], dst)
+    reported(c["table"], c["seqlens"], torch.full_like(dst, c["k"].shape[0]))
+    reported(c["table"], torch.tensor([100, 113], dtype=torch.int32, device="cuda"), dst, torch.rand(2, 1, 200, device="cuda"))
+    reported(c["table"], c["seqlens"], dst[:, :1].contiguous())                # no room for 40 tokens
+    reported(c["table"], c["seqlens"], dst, w[..., :50].contiguous())          # weights of fewer positions
+
+
+# ---- together ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("int8", [False, True])
+def test_decoding_loop(int8):
+    """Prompts go in, tokens are decoded, the cache is shortened and decoding goes on: the whole run against one that keeps its rows in
+    plain lists."""
+    Hq, Hkv, D, page, budget = 8, 2, 64, 16, 48
+    prompts, steps = [50, 7, 64], 12
+    B, ld, width = len(prompts), 96, 6
+    g = torch.Generator().manual_seed(11)
+    blocks = 2 * B * width
+    k = torch.zeros(blocks, page, Hkv, D, dtype=torch.int8 if int8 else torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    ks, vs = (torch.zeros(blocks, page, Hkv, device="cuda"), torch.zeros(blocks, page, Hkv, device="cuda")) if int8 else (None, None)
+    tables = torch.randperm(blocks, generator=g).int().view(2, B, width).cuda()
+    weights = torch.full((B, Hkv, ld), float("nan"), device="cuda")               # nothing of it may show
+    lengths = list(prompts)
+    rows = [{"k": [[] for _ in range(Hkv)], "v": [[] for _ in range(Hkv)], "w": [[] for _ in range(Hkv)]} for _ in range(B)]
+
+    def stored(x):                                        # what the cache holds for a row, 64 bits
+        if not int8:
+            return x.double()
+        codes, s = inputs.quantize_rows_int8(x.contiguous().view(torch.int16).numpy().view(np.uint16))
+        return torch.from_numpy(codes).double() * torch.from_numpy(np.asarray(s)).double()[..., None]
+
+    def append(new_counts, table):
+        cu = [0]
+        for n in new_counts:
+            cu.append(cu[-1] + n)
+        kn, vn = (torch.randn(cu[-1], Hkv, D, generator=g).to(torch.bfloat16) for _ in range(2))
+        binding.kv_append_paged(kn.cuda(), vn.cuda(), k, v, ks, vs, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"),
+                                torch.tensor(cu, dtype=torch.int32, device="cuda"), weights=weights)
+        for b in range(B):
+            for i in range(cu[b], cu[b + 1]):
+                sk, sv = stored(kn[i]), stored(vn[i])
+                for h in range(Hkv):
+                    rows[b]["k"][h].append(sk[h])
+                    rows[b]["v"][h].append(sv[h])
+                    rows[b]["w"][h].append(0.0)
+
+    at = 0
+    append(prompts, tables[at])
+    for step in range(steps):
+        for b in range(B):
+            lengths[b] += 1
+        append([1] * B, tables[at])
+        q = torch.randn(B, Hq, D, generator=g).to(torch.bfloat16)
+        got = binding.attn_decode_paged(q.cuda(), k, v, ks, vs, tables[at], torch.tensor(lengths, dtype=torch.int32, device="cuda"), 0.125,
+                                        weights=weights)
+        for b in range(B):
+            for h in range(Hkv):
+                K, V = torch.stack(rows[b]["k"][h]), torch.stack(rows[b]["v"][h])
+                heads = slice(h * Hq // Hkv, (h + 1) * Hq // Hkv)
+                p = torch.softmax(q[b, heads].double() @ K.T * 0.125, -1)
+                want, mass = p @ V, p @ V.abs()
+                # two roundings to BF16; the FP32 part (about (D + 8) 2^-23 sum |q k| scale, twice) stays below 2^-12 here
+                bound = HALF_BF16 * want.abs() + (HALF_BF16 + 2.0 ** -12) * mass
+                assert ((got[b, heads].double().cpu() - want).abs() <= bound).all()
+                rows[b]["w"][h] = [x + y for x, y in zip(rows[b]["w"][h], p.sum(0).tolist())]
+                now = weights[b, h, :lengths[b]].double().cpu()
+                ref = torch.tensor(rows[b]["w"][h])
+                assert ((now - ref).abs() <= 2.0 ** -12 * ref.abs() + 1e-12).all()
+        if step % 4 == 3:
+            old = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+            new_seqlens, new_weights, kept = binding.kv_evict_paged(k, v, ks, vs, tables[at], old, weights, budget, tables[1 - at], recent=8, sinks=2)
+            # which tokens stay goes by the weights as they are: compared exactly, from the same numbers
+            for b in range(B):
+                for h in range(Hkv):
+                    stay = evicted(weights[b, h].tolist(), lengths[b], budget, 8, 2)
+                    assert kept[b, h, :len(stay)].tolist() == stay
+                    for x in ("k", "v", "w"):
+                        rows[b][x][h] = [rows[b][x][h][j] for j in stay]
+            lengths = new_seqlens.tolist()
+            assert lengths == [len(rows[b]["k"][0]) for b in range(B)]
+            weights, at = new_weights, 1 - at
+            # the pages that were left are anybody's again
+            for pool in (k, v):
+                pool[tables[1 - at].flatten().long()] = 127 if int8 else float("nan")
+    binding.last_device_status()
+
+
+def test_eviction_replays_from_a_graph():
+    c, dst = _evict_case([600, 130], 2, 64, 64, 16, 100, True, seed=12)
+    w = torch.rand(2, 2, 600, generator=torch.Generator().manual_seed(12)).cuda()
+    pools = [(c[x], c[x].cpu().clone()) for x in ("k", "v", "k_scale", "v_scale")]
+    got = binding.kv_evict_paged(*_args(c), w, 100, dst, recent=9, sinks=1)
+    new_seqlens, new_weights, kept = got
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        binding.kv_evict_paged(*_args(c), w, 100, dst, recent=9, sinks=1, new_seqlens=new_seqlens, new_weights=new_weights, kept=kept)
+    w.copy_(torch.rand(2, 2, 600, generator=torch.Generator().manual_seed(13)))
+    graph.replay()
+    binding.last_device_status()
+    _check_evicted(c, dst, w, got, 100, 9, 1, pools)

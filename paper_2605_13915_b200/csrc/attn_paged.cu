@@ -19,8 +19,10 @@
 // A sequence inside one run is finished there; only the first and the last of a run can be cut, so a CTA leaves at most two
 // partial results, whatever the lengths are, and a second kernel joins those and turns the scores into weights.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "paged.cuh"
 
@@ -30,7 +32,7 @@ namespace {
 
 constexpr int kPWarps = 4;
 constexpr int kPThreads = 32 * kPWarps;
-constexpr int kPRows = 16;                  // head slots of a CTA (MMA rows)
+constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
 
 struct PagedAttnParams {
@@ -46,14 +48,16 @@ struct PagedAttnParams {
   float* lse;
   float* weights;
   int64_t ld, score_ld;
+  int score_heads;            // heads of a position's scores: G, made even
+  int slots;                  // head slots of a CTA, 8 or 16
   // workspace
   float* part;                // [CTA][2][rows][Dv]: unnormalised outputs
   float* part_ml;             // [CTA][2][rows][2]: maximum (log2) and sum
   int2* tail;                 // [CTA] what the join does for it: {sequence cut at the end of its run or -1, last run of that sequence}
   int2* seq_runs;             // [B] {first, last run}
   float* lse2;                // [B, Hq] log2-sum of uncut sequences
-  float* scores;              // [B, Hq, score_ld] log2 scores
-  int part_rows;              // rows of a partial result: min(G, 16)
+  float* scores;              // [B, Hkv, score_ld, score_heads] log2 scores
+  int part_rows;              // rows of a partial result: min(G, slots)
   int join_weight_ctas;       // CTAs of the join per (sequence, KV head)
   unsigned* status;
 };
@@ -78,44 +82,58 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
-__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+template <bool kHalfs>      // FP16 or BF16 operands
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], const uint2& b) {
+  if constexpr (kHalfs)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// bytes kLo and kHi of r (two's complement) as a BF16 pair
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {       // of an 8 x 8 matrix of 16-bit values over the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// bytes kLo and kHi of u, each a code plus 128, as an FP16 pair of the codes: 1024 + u has the byte as its lowest bits
 template <int kLo, int kHi>
-__device__ __forceinline__ uint32_t int8_pair(uint32_t r) {
-  const uint32_t t = __byte_perm(r, 0x43u, 0x4040 | kLo | (kHi << 8));        // each byte below 0x43: 128 + (x & 127), and the sign as bit 7
-  const uint32_t low = t & 0xFF7FFF7Fu, sign = t & 0xFF80FF80u;
-  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&low), *reinterpret_cast<const __nv_bfloat162*>(&sign));
+__device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
+  const uint32_t t = __byte_perm(u, 0x64646464u, 0x4040 | kLo | (kHi << 8));
+  const uint32_t off = 0x64806480u;                                // 1152
+  const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&t), *reinterpret_cast<const __half2*>(&off));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 
-// DP: D and Dv rounded up to 64, 128 or 256.  A tile of a warp: 8 KB of keys and values where that is 16 or 32 tokens; three of them in
-// flight and two CTAs an SM put 200 KB of loads under way, four times what the latency of a loaded memory asks for.
-template <bool kInt8, int DP>
+// DP: D and Dv rounded up to 64, 128 or 256; kHeads: head slots of a CTA, 8 or 16.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB of
+// keys and values; the rings of all CTAs of an SM together hold about 200 KB.
+template <bool kInt8, int DP, int kHeads>
 struct Shape {
   static constexpr int kEs = kInt8 ? 1 : 2;
-  static constexpr int kTok = (DP == 64 || (kInt8 && DP == 128)) ? 32 : 16;
+  static constexpr int kTok = kInt8 && DP == 64 ? 32 : 16;
   static constexpr int kRow = DP * kEs;                         // bytes of a row in shared memory
   static constexpr int kHalf = kTok * kRow;                     // keys, then values
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
-  static constexpr int kStages = kInt8 ? (DP == 64 ? 4 : (DP == 256 ? 6 : 3)) : 3;
-  static constexpr int kCtasPerSm = DP == 256 ? 1 : 2;
-  static constexpr bool kQInSmem = DP == 256;                   // (64 registers of query fragments beside 128 of outputs are too many)
-  static constexpr int kQRow = DP * 2 + 16;                     // bytes: rows 16 bytes apart in the banks
+  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kHalf >= 4096 ? 2 : (kHeads == 8 ? 4 : 3));
+  static constexpr int kStages = kHeads == 16 && kHalf <= 2048 ? 4 : (kHeads == 16 && kInt8 && DP == 256 ? 2 : 3);
+  static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
   static constexpr int kRing = kPWarps * kStages * kStage;
-  static constexpr int kOut = kPRows * (DP + 4) * 4;            // where the warps' outputs meet
-  static constexpr int kSmem = kRing + kOut + (kQInSmem ? kPRows * kQRow : 0);
+  static constexpr int kORow = DP + 4;
+  static constexpr int kOut = kHeads * kORow * 4;               // where the warps' outputs meet
+  static constexpr int kSmem = kRing + kOut + (kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0);
   static constexpr int kTile = kPWarps * kTok;                  // tokens of a CTA's tile
-  static_assert(kCtasPerSm * (kSmem + 2048) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
+  static_assert(kCtasPerSm * (kSmem + 1600) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
 };
 
 // 16-byte chunk c of row r, so that the eight rows of a matrix lie in different banks
@@ -129,18 +147,19 @@ __device__ __forceinline__ int seq_len(const PagedAttnParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(n < 0 ? 0 : n), p.cap));
 }
 
-template <bool kInt8, int DP>
-__global__ void __launch_bounds__(kPThreads, (Shape<kInt8, DP>::kCtasPerSm))
+template <bool kInt8, int DP, int kHeads>
+__global__ void __launch_bounds__(kPThreads, (Shape<kInt8, DP, kHeads>::kCtasPerSm))
 attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
-  using S = Shape<kInt8, DP>;
+  using S = Shape<kInt8, DP, kHeads>;
+  constexpr int NT = kHeads / 8;                        // column tiles of heads
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int scan_buf[kPWarps];
   __shared__ int start_buf[2];
-  __shared__ float ml[2][kPWarps][kPRows];
+  __shared__ float ml[2][kPWarps][kHeads];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
-  const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kPRows;        // first head of the group within the KV head
-  const int nh = min(p.G - h0, kPRows);
+  const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kHeads;        // first head of the group within the KV head
+  const int nh = min(p.G - h0, kHeads);
   const int64_t head0 = static_cast<int64_t>(hk) * p.G + h0;
 
   pdl_wait_primary();
@@ -280,53 +299,85 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   for (int s = 0; s < S::kStages - 1; ++s) issue(s);
 
   // ---- the arithmetic ----
-  const int row = lane >> 2, quad = lane & 3;           // rows `row` and `row` + 8 of the fragments
-  uint8_t* sm_q = smem + S::kRing + S::kOut;
+  const int row = lane >> 2, quad = lane & 3;           // a thread has tokens (or values of d) `row`, `row` + 8 and heads 2 quad, 2 quad + 1
   float* sm_o = reinterpret_cast<float*>(smem + S::kRing);
+  uint2* sm_q = reinterpret_cast<uint2*>(smem + S::kRing + S::kOut);
   constexpr int kSteps = DP / 16;
-  uint32_t qf[S::kQInSmem ? 1 : kSteps][4];
-  float o[DP / 8][4];
-  float m0, m1, l0, l1;
-  const int k_steps = (p.c.D + 15) / 16;
+  uint2 qf[S::kQInSmem ? 1 : kSteps][NT];
+  float o[NT][DP / 16][4];
+  float m[NT][2], l[NT][2], f[NT][2];                   // f: from products to log2 scores
+  const int k_steps = (p.c.D + 15) / 16, v_steps = (p.c.Dv + 15) / 16;
 
+  // The query as column fragments: head `row` of each tile.  INT8: of 16 values of d a thread's bytes are 4 quad ... 4 quad + 3, so the
+  // query is taken in that order too, and goes into FP16 scaled by a power of two that brings its largest value to 2^14 ... 2^15: what
+  // is 2^-29 of that or more stays exact, the rest is off by 2^-40 of it at most.
   auto load_q = [&]() {
     const uint16_t* q = p.q + static_cast<int64_t>(cur.b) * p.q_ld + head0 * p.c.D;
+    auto raw = [&](int s, int n) {
+      uint2 v = make_uint2(0, 0);
+      const int h = n * 8 + row;
+      const uint16_t* at = q + h * p.c.D + s * 16;
+      if (h < nh) {
+        if constexpr (kInt8) {
+          if (s * 16 + 4 * quad < p.c.D) v = *reinterpret_cast<const uint2*>(at + 4 * quad);
+        } else {
+          if (s * 16 + 2 * quad < p.c.D) v.x = *reinterpret_cast<const uint32_t*>(at + 2 * quad);
+          if (s * 16 + 2 * quad + 8 < p.c.D) v.y = *reinterpret_cast<const uint32_t*>(at + 2 * quad + 8);
+        }
+      }
+      return v;
+    };
+    float up[NT];
+    if constexpr (kInt8) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        uint32_t big = 0;                               // of |x| as BF16 bits, which grow with the value
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const uint2 v = raw(s, n);
+          if constexpr (!S::kQInSmem) qf[s][n] = v;
+          big = __vmaxu2(big, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu));
+        }
+        big = max(big & 0xFFFFu, big >> 16);
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // the exponent of the largest value, from -126 (or less: taken as that) to 127
+        const int e = max(static_cast<int>(big >> 7), 1) - 127;
+        // 2^(14 - e), cut to what a float holds: then the values are small, and stay exact as well
+        up[n] = __uint_as_float(static_cast<uint32_t>(min(14 - e, 126) + 127) << 23);
+        const float down = p.scale2 / up[n];
+        f[n][0] = __shfl_sync(0xffffffffu, down, 8 * quad);
+        f[n][1] = __shfl_sync(0xffffffffu, down, 8 * quad + 4);
+      }
+    }
+    auto fragment = [&](uint2 v, int n) {
+      if constexpr (kInt8) {
+        return make_uint2(pack_f16(__uint_as_float(v.x << 16) * up[n], __uint_as_float(v.x & 0xFFFF0000u) * up[n]),
+                          pack_f16(__uint_as_float(v.y << 16) * up[n], __uint_as_float(v.y & 0xFFFF0000u) * up[n]));
+      } else {
+        return v;
+      }
+    };
     if constexpr (S::kQInSmem) {
-      for (int i = threadIdx.x; i < kPRows * (DP / 8); i += kPThreads) {
-        const int r = i / (DP / 8), c = i % (DP / 8);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < nh && c * 8 < p.c.D) v = *reinterpret_cast<const uint4*>(q + r * p.c.D + c * 8);
-        *reinterpret_cast<uint4*>(sm_q + r * S::kQRow + c * 16) = v;
+      for (int s = warp; s < kSteps; s += kPWarps) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sm_q[(s * NT + n) * 32 + lane] = fragment(raw(s, n), n);
       }
       __syncthreads();
     } else {
-      // INT8: of 16 values of d a thread's bytes are 4 quad ... 4 quad + 3, so the query is taken in that order too
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = row + (j & 1) * 8;
-          const int d = s * 16 + (kInt8 ? 4 * quad + (j >> 1) * 2 : 2 * quad + (j >> 1) * 8);
-          qf[s][j] = (r < nh && d < p.c.D) ? *reinterpret_cast<const uint32_t*>(q + r * p.c.D + d) : 0u;
-        }
+        for (int s = 0; s < kSteps; ++s) qf[s][n] = fragment(kInt8 ? qf[s][n] : raw(s, n), n);
       }
     }
   };
-  auto q_fragment = [&](int s, uint32_t (&a)[4]) {
-    if constexpr (!S::kQInSmem) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) a[j] = qf[s][j];
-    } else if constexpr (kInt8) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint2 v = *reinterpret_cast<const uint2*>(sm_q + (row + j * 8) * S::kQRow + s * 32 + quad * 8);
-        a[j] = v.x;
-        a[j + 2] = v.y;
-      }
-    } else {
-      ldsm4(a, smem_u32(sm_q) + (lane & 15) * S::kQRow + s * 32 + (lane >> 4) * 16);
-    }
+  auto q_fragment = [&](int s, int n) {
+    if constexpr (S::kQInSmem) return sm_q[(s * NT + n) * 32 + lane];
+    else return qf[s][n];
   };
+#pragma unroll
+  for (int n = 0; n < NT; ++n) f[n][0] = f[n][1] = p.scale2;
 
   int it = 0;
   while (cur.left > 0) {
@@ -335,10 +386,15 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     const int seg = min(cur.tiles - cur.tile, cur.left);
     const int b = cur.b, L = cur.L;
     load_q();
-    m0 = m1 = -INFINITY;
-    l0 = l1 = 0.0f;
 #pragma unroll
-    for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
+    }
+    // INT8: a power of two that no value's scale so far exceeds (2^-111 at least, so that 2^15 / vref is finite); outputs are in units of vref / 2^15
+    float vref = 3.851859888774472e-34f;
 
     for (int t = 0; t < seg; ++t, ++it) {
       const int stage = it % S::kStages;
@@ -350,143 +406,160 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       if (pos0 >= L) continue;                          // (uniform in the warp)
       const uint32_t sk = ring_u + stage * S::kStage, sv = sk + S::kHalf;
       const float* scales = reinterpret_cast<const float*>(ring + stage * S::kStage + 2 * S::kHalf);
+      constexpr int kGroups = S::kTok / 16;
 
-      // scores
-      float s[S::kTok / 8][4];
+      // scores of 16 tokens (rows) and 8 heads (columns) a fragment
+      float s[kGroups][NT][4];
 #pragma unroll
-      for (int n = 0; n < S::kTok / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
-      if constexpr (kInt8) {
+      for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
-        for (int c4 = 0; c4 < DP / 64; ++c4) {
-          if (c4 * 4 < k_steps) {
-            uint32_t a[4][4];
+        for (int n = 0; n < NT; ++n) s[g][n][0] = s[g][n][1] = s[g][n][2] = s[g][n][3] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q_fragment(c4 * 4 + i, a[i]);
-#pragma unroll
-            for (int n = 0; n < S::kTok / 8; ++n) {
-              uint32_t r[4];
-              ldsm4(r, sk + swz<S::kRow>(n * 8 + (lane & 7), c4 * 4 + (lane >> 3)));
-#pragma unroll
-              for (int i = 0; i < 4; ++i) mma_bf16(s[n], a[i], int8_pair<0, 1>(r[i]), int8_pair<2, 3>(r[i]));
-            }
-          }
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < kSteps; ++c) {
+        for (int c = 0; c < kSteps; c += kInt8 ? 2 : 1) {
           if (c < k_steps) {
-            uint32_t a[4];
-            q_fragment(c, a);
-#pragma unroll
-            for (int n = 0; n < S::kTok / 8; n += 2) {
-              uint32_t r[4];
-              ldsm4(r, sk + swz<S::kRow>(n * 8 + ((lane >> 4) << 3) + (lane & 7), 2 * c + ((lane >> 3) & 1)));
-              mma_bf16(s[n], a, r[0], r[1]);
-              mma_bf16(s[n + 1], a, r[2], r[3]);
-            }
-          }
-        }
-      }
-
-      // softmax
-      float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-      for (int n = 0; n < S::kTok / 8; ++n) {
-        float f0 = p.scale2, f1 = p.scale2;
-        if constexpr (kInt8) {
-          const float2 ks = *reinterpret_cast<const float2*>(scales + n * 8 + 2 * quad);
-          f0 *= ks.x;
-          f1 *= ks.y;
-        }
-        s[n][0] *= f0;
-        s[n][1] *= f1;
-        s[n][2] *= f0;
-        s[n][3] *= f1;
-      }
-      if (pos0 + S::kTok > L) {
-#pragma unroll
-        for (int n = 0; n < S::kTok / 8; ++n) {
-          const int pos = pos0 + n * 8 + 2 * quad;
-          if (pos >= L) s[n][0] = s[n][2] = -INFINITY;
-          if (pos + 1 >= L) s[n][1] = s[n][3] = -INFINITY;
-        }
-      }
-      if (p.weights) {
-        float* dst = p.scores + (static_cast<int64_t>(b) * p.Hq + head0 + row) * p.score_ld + pos0 + 2 * quad;
-#pragma unroll
-        for (int n = 0; n < S::kTok / 8; ++n) {
-          if (pos0 + n * 8 + 2 * quad < L) {
-            if (row < nh) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(s[n][0], s[n][1]);
-            if (row + 8 < nh) *reinterpret_cast<float2*>(dst + 8 * p.score_ld + n * 8) = make_float2(s[n][2], s[n][3]);
-          }
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < S::kTok / 8; ++n) {
-        mx0 = fmaxf(mx0, fmaxf(s[n][0], s[n][1]));
-        mx1 = fmaxf(mx1, fmaxf(s[n][2], s[n][3]));
-      }
-#pragma unroll
-      for (int d = 1; d < 4; d <<= 1) {
-        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
-        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
-      }
-      mx0 = fmaxf(mx0, m0);
-      mx1 = fmaxf(mx1, m1);
-      if (__any_sync(0xffffffffu, mx0 != m0 || mx1 != m1)) {
-        const float r0 = mx0 == -INFINITY ? 1.0f : ex2(m0 - mx0), r1 = mx1 == -INFINITY ? 1.0f : ex2(m1 - mx1);
-        m0 = mx0;
-        m1 = mx1;
-        l0 *= r0;
-        l1 *= r1;
-#pragma unroll
-        for (int i = 0; i < DP / 8; ++i) {
-          o[i][0] *= r0;
-          o[i][1] *= r0;
-          o[i][2] *= r1;
-          o[i][3] *= r1;
-        }
-      }
-      const float e0 = m0 == -INFINITY ? 0.0f : m0, e1 = m1 == -INFINITY ? 0.0f : m1;
-#pragma unroll
-      for (int n = 0; n < S::kTok / 8; ++n) {
-        s[n][0] = ex2(s[n][0] - e0);
-        s[n][1] = ex2(s[n][1] - e0);
-        s[n][2] = ex2(s[n][2] - e1);
-        s[n][3] = ex2(s[n][3] - e1);
-        l0 += s[n][0] + s[n][1];
-        l1 += s[n][2] + s[n][3];
-      }
-
-      // product with v, 16 tokens at a time
-#pragma unroll
-      for (int g = 0; g < S::kTok / 16; ++g) {
-        if constexpr (kInt8) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float2 vs = *reinterpret_cast<const float2*>(scales + S::kTok + (2 * g + j) * 8 + 2 * quad);
-            s[2 * g + j][0] *= vs.x;
-            s[2 * g + j][1] *= vs.y;
-            s[2 * g + j][2] *= vs.x;
-            s[2 * g + j][3] *= vs.y;
-          }
-        }
-        const uint32_t a[4] = {pack_bf16(s[2 * g][0], s[2 * g][1]), pack_bf16(s[2 * g][2], s[2 * g][3]),
-                               pack_bf16(s[2 * g + 1][0], s[2 * g + 1][1]), pack_bf16(s[2 * g + 1][2], s[2 * g + 1][3])};
-#pragma unroll
-        for (int c = 0; c < kChunks; c += 2) {
-          if (c < v_chunks) {
             uint32_t r[4];
-            ldsm4_t(r, sv + swz<S::kRow>(g * 16 + (lane & 15), c + (lane >> 4)));
-            if constexpr (kInt8) {      // a register holds two tokens of an even and the next odd value of d
+            ldsm4(r, sk + swz<S::kRow>(g * 16 + (lane & 15), (kInt8 ? c : 2 * c) + (lane >> 4)));
+            if constexpr (kInt8) {                      // a register: four codes of a token; two registers a step
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                mma_bf16(o[2 * (c + j)], a, int8_pair<0, 2>(r[2 * j]), int8_pair<0, 2>(r[2 * j + 1]));
-                mma_bf16(o[2 * (c + j) + 1], a, int8_pair<1, 3>(r[2 * j]), int8_pair<1, 3>(r[2 * j + 1]));
+                const uint32_t x = r[2 * j] ^ 0x80808080u, y = r[2 * j + 1] ^ 0x80808080u;
+                const uint32_t a[4] = {codes_f16<0, 1>(x), codes_f16<0, 1>(y), codes_f16<2, 3>(x), codes_f16<2, 3>(y)};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16<true>(s[g][n], a, q_fragment(c + j, n));
               }
             } else {
-              mma_bf16(o[c], a, r[0], r[1]);
-              mma_bf16(o[c + 1], a, r[2], r[3]);
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma16<false>(s[g][n], r, q_fragment(c, n));
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        float k0 = 1.0f, k1 = 1.0f;
+        if constexpr (kInt8) {
+          k0 = scales[g * 16 + row];
+          k1 = scales[g * 16 + row + 8];
+        }
+        const bool out0 = pos0 + g * 16 + row >= L, out1 = pos0 + g * 16 + row + 8 >= L;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s[g][n][e] = out0 ? -INFINITY : s[g][n][e] * (f[n][e] * k0);
+            s[g][n][2 + e] = out1 ? -INFINITY : s[g][n][2 + e] * (f[n][e] * k1);
+          }
+        }
+        if (p.weights) {
+          float* dst = p.scores + ((static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + pos0 + g * 16 + row) * p.score_heads + h0 + 2 * quad;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if (n * 8 + 2 * quad < nh) {
+              if (!out0) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(s[g][n][0], s[g][n][1]);
+              if (!out1) *reinterpret_cast<float2*>(dst + 8 * p.score_heads + n * 8) = make_float2(s[g][n][2], s[g][n][3]);
+            }
+          }
+        }
+      }
+
+      // softmax; the maximum of a head moves rarely, and only then do the lanes ask each other
+      float mx[NT][2];
+      bool moved = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          mx[n][e] = fmaxf(s[0][n][e], s[0][n][2 + e]);
+#pragma unroll
+          for (int g = 1; g < kGroups; ++g) mx[n][e] = fmaxf(mx[n][e], fmaxf(s[g][n][e], s[g][n][2 + e]));
+          moved = moved || mx[n][e] > m[n][e];
+        }
+      }
+      float vs[kGroups][2];
+      float vnew = vref;
+      if constexpr (kInt8) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(scales[S::kTok + (lane & (S::kTok - 1))]) & 0x7FFFFFFFu);
+        if (top > __float_as_uint(vref)) {              // (uniform) the next power of two
+          vnew = __uint_as_float(min((top + 0x007FFFFFu) & 0x7F800000u, 0x7F000000u));
+          moved = true;
+        }
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+        const float vr = kInt8 ? vref / vnew : 1.0f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], d));
+            mx[n][e] = fmaxf(mx[n][e], m[n][e]);
+            const float r = mx[n][e] == -INFINITY ? 1.0f : ex2(m[n][e] - mx[n][e]);
+            m[n][e] = mx[n][e];
+            l[n][e] *= r;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+              o[n][i][e] *= r * vr;
+              o[n][i][2 + e] *= r * vr;
+            }
+          }
+        }
+        vref = vnew;
+      }
+      if constexpr (kInt8) {
+        const float c = 32768.0f / vref;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          vs[g][0] = scales[S::kTok + g * 16 + row] * c;
+          vs[g][1] = scales[S::kTok + g * 16 + row + 8] * c;
+        }
+      }
+      // Probabilities as column fragments of the product with v: the transposes of the score fragments.  INT8: times the value's scale,
+      // in FP16 (11 bits).  BF16: the 8 bits of one BF16 would double the error of the result, so what they leave out goes in too.
+      uint2 ph[kGroups][NT], pl[kGroups][NT];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float mm = m[n][e & 1];
+            x[e] = ex2(s[g][n][e] - (mm == -INFINITY ? 0.0f : mm));
+            l[n][e & 1] += x[e];
+          }
+          if constexpr (kInt8) {
+            ph[g][n] = make_uint2(transposed(pack_f16(x[0] * vs[g][0], x[1] * vs[g][0])), transposed(pack_f16(x[2] * vs[g][1], x[3] * vs[g][1])));
+          } else {
+            const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
+            ph[g][n] = make_uint2(transposed(a), transposed(c));
+            pl[g][n] = make_uint2(transposed(pack_bf16(x[0] - __uint_as_float(a << 16), x[1] - __uint_as_float(a & 0xFFFF0000u))),
+                                  transposed(pack_bf16(x[2] - __uint_as_float(c << 16), x[3] - __uint_as_float(c & 0xFFFF0000u))));
+          }
+        }
+      }
+      // 16 values of d (rows) and 8 heads a fragment
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+        for (int c = 0; c < DP / 16; c += kInt8 ? 2 : 1) {
+          if (c < v_steps) {
+            uint32_t r[4];
+            if constexpr (kInt8) {                      // a register: two tokens of an even and the next odd value of d
+              ldsm4_t(r, sv + swz<S::kRow>(g * 16 + (lane & 15), c + (lane >> 4)));
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t x = r[2 * j] ^ 0x80808080u, y = r[2 * j + 1] ^ 0x80808080u;
+                const uint32_t a[4] = {codes_f16<0, 2>(x), codes_f16<1, 3>(x), codes_f16<0, 2>(y), codes_f16<1, 3>(y)};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma16<true>(o[n][c + j], a, ph[g][n]);
+              }
+            } else {
+              ldsm4_t(r, sv + swz<S::kRow>(g * 16 + ((lane >> 4) << 3) + (lane & 7), 2 * c + ((lane >> 3) & 1)));
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                mma16<false>(o[n][c], r, ph[g][n]);
+                mma16<false>(o[n][c], r, pl[g][n]);
+              }
             }
           }
         }
@@ -495,54 +568,58 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 
     // ---- the segment's end: the warps meet ----
 #pragma unroll
-    for (int d = 1; d < 4; d <<= 1) {
-      l0 += __shfl_xor_sync(0xffffffffu, l0, d);
-      l1 += __shfl_xor_sync(0xffffffffu, l1, d);
-    }
-    if (quad == 0) {
-      ml[0][warp][row] = m0;
-      ml[0][warp][row + 8] = m1;
-      ml[1][warp][row] = l0;
-      ml[1][warp][row + 8] = l1;
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+        if (row == 0) {
+          ml[0][warp][n * 8 + 2 * quad + e] = m[n][e];
+          ml[1][warp][n * 8 + 2 * quad + e] = l[n][e];
+        }
+      }
     }
     __syncthreads();
-    auto joined = [&](int r, float* m, float* l) {
-      float mm = ml[0][0][r];
+    auto joined = [&](int h, float* mh, float* lh) {
+      float mm = ml[0][0][h];
 #pragma unroll
-      for (int w = 1; w < kPWarps; ++w) mm = fmaxf(mm, ml[0][w][r]);
+      for (int w = 1; w < kPWarps; ++w) mm = fmaxf(mm, ml[0][w][h]);
       float ll = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kPWarps; ++w) ll += ml[1][w][r] * (ml[0][w][r] == -INFINITY ? 0.0f : ex2(ml[0][w][r] - mm));
-      *m = mm;
-      *l = ll;
+      for (int w = 0; w < kPWarps; ++w) ll += ml[1][w][h] * (ml[0][w][h] == -INFINITY ? 0.0f : ex2(ml[0][w][h] - mm));
+      *mh = mm;
+      *lh = ll;
     };
-    float M0, M1, L0, L1;
-    joined(row, &M0, &L0);
-    joined(row + 8, &M1, &L1);
-    const float f0 = m0 == -INFINITY ? 0.0f : ex2(m0 - M0), f1 = m1 == -INFINITY ? 0.0f : ex2(m1 - M1);
-    constexpr int kORow = DP + 4;
+    float out_f[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float mh, lh;
+        joined(n * 8 + 2 * quad + e, &mh, &lh);
+        out_f[n][e] = m[n][e] == -INFINITY ? 0.0f : ex2(m[n][e] - mh) * (kInt8 ? vref * 3.0517578125e-05f : 1.0f);
+      }
+    }
+    constexpr int kORow = S::kORow;
     for (int w = 0; w < kPWarps; ++w) {          // one after the other: the order of the sums is fixed
       if (w == warp) {
 #pragma unroll
-        for (int i = 0; i < DP / 8; i += 2) {
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float f = j ? f1 : f0;
-            const int r = row + 8 * j;
-            if (r < nh) {
-              float x[4] = {o[i][2 * j] * f, o[i][2 * j + 1] * f, o[i + 1][2 * j] * f, o[i + 1][2 * j + 1] * f};
-              if constexpr (kInt8) {             // columns 2 quad, 2 quad + 1 of a pair of fragments are four values in a row
-                float4* dst = reinterpret_cast<float4*>(sm_o + r * kORow + i * 8 + 4 * quad);
-                float4 v = make_float4(x[0], x[2], x[1], x[3]);
-                if (w > 0) { const float4 y = *dst; v.x += y.x; v.y += y.y; v.z += y.z; v.w += y.w; }
-                *dst = v;
-              } else {
+          for (int e = 0; e < 2; ++e) {
+            if (n * 8 + 2 * quad + e < nh) {
+              float* dst = sm_o + (n * 8 + 2 * quad + e) * kORow;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  float2* dst = reinterpret_cast<float2*>(sm_o + r * kORow + (i + k) * 8 + 2 * quad);
-                  float2 v = make_float2(x[2 * k], x[2 * k + 1]);
-                  if (w > 0) { const float2 y = *dst; v.x += y.x; v.y += y.y; }
-                  *dst = v;
+              for (int i = 0; i < DP / 16; ++i) {
+                const float x = o[n][i][e] * out_f[n][e], y = o[n][i][2 + e] * out_f[n][e];
+                if constexpr (kInt8) {
+                  float2* at = reinterpret_cast<float2*>(dst + i * 16 + 2 * row);
+                  const float2 was = w > 0 ? *at : make_float2(0.0f, 0.0f);
+                  *at = make_float2(was.x + x, was.y + y);
+                } else {
+                  float* at = dst + i * 16 + row;
+                  at[0] = (w > 0 ? at[0] : 0.0f) + x;
+                  at[8] = (w > 0 ? at[8] : 0.0f) + y;
                 }
               }
             }
@@ -561,15 +638,15 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     if (from_start && to_end) {
       for (int i = threadIdx.x; i < nh * vecs; i += kPThreads) {
         const int r = i / vecs, d = (i - r * vecs) * 4;
-        float m, l;
-        joined(r, &m, &l);
-        const float inv = 1.0f / l;
+        float mh, lh;
+        joined(r, &mh, &lh);
+        const float inv = 1.0f / lh;
         const float4 v = *reinterpret_cast<const float4*>(sm_o + r * kORow + d);
         const uint2 w = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
         const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + r;
         *reinterpret_cast<uint2*>(p.out + out_row * Dv + d) = w;
         if (d == 0) {
-          const float lg = m + log2f(l);
+          const float lg = mh + log2f(lh);
           if (p.lse) p.lse[out_row] = lg * 0.6931471805599453f;
           if (p.weights) p.lse2[out_row] = lg;
         }
@@ -580,9 +657,9 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         const int r = i / vecs, d = (i - r * vecs) * 4;
         *reinterpret_cast<float4*>(p.part + (slot * p.part_rows + r) * Dv + d) = *reinterpret_cast<const float4*>(sm_o + r * kORow + d);
         if (d == 0) {
-          float m, l;
-          joined(r, &m, &l);
-          *reinterpret_cast<float2*>(p.part_ml + (slot * p.part_rows + r) * 2) = make_float2(m, l);
+          float mh, lh;
+          joined(r, &mh, &lh);
+          *reinterpret_cast<float2*>(p.part_ml + (slot * p.part_rows + r) * 2) = make_float2(mh, lh);
         }
       }
       if (from_start && threadIdx.x == 0) {
@@ -599,7 +676,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 // (the other CTAs: (sequence, KV head) x share of the positions) from the scores that the first kernel left.
 __global__ void __launch_bounds__(kJoinThreads)
 attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
-  __shared__ float f[kPRows * 2];
+  __shared__ float f[kMaxSlots * 2];
   __shared__ float4 sums[kJoinThreads];
   extern __shared__ float lse2_sm[];             // [G]
   pdl_wait_primary();
@@ -610,7 +687,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
     const int2 tail = p.tail[blockIdx.x];
     if (tail.x < 0) return;
-    const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kPRows, nh = min(p.G - h0, kPRows);
+    const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
     const int n = tail.y - run + 1;              // pieces: slot 1 of this CTA, slot 0 of the runs after it
     auto slot = [&](int i) { return i == 0 ? static_cast<int64_t>(blockIdx.x) * 2 + 1 : (static_cast<int64_t>(run + i) * p.U + unit) * 2; };
     for (int r = tid >> 5; r < nh; r += kJoinThreads / 32) {       // a warp for each row's maximum and sum
@@ -630,7 +707,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
       }
       if ((tid & 31) == 0) {
         f[r] = m == -INFINITY ? 0.0f : m;
-        f[kPRows + r] = 1.0f / l;
+        f[kMaxSlots + r] = 1.0f / l;
         if (p.lse) p.lse[static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0 + r] = (m + log2f(l)) * 0.6931471805599453f;
       }
     }
@@ -662,7 +739,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
           acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
         }
         const int r = item / vecs, d = (item - r * vecs) * 4;
-        const float inv = f[kPRows + r];
+        const float inv = f[kMaxSlots + r];
         *reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0 + r) * p.c.Dv + d) =
             make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
       }
@@ -681,7 +758,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     if (span.x == span.y) {
       lg = p.lse2[static_cast<int64_t>(b) * p.Hq + hk * p.G + g];
     } else {
-      const int unit = hk * p.groups + g / kPRows, r = g % kPRows;
+      const int unit = hk * p.groups + g / p.slots, r = g % p.slots;
       float m = -INFINITY, l = 0.0f;
       for (int i = tid & 31; i <= span.y - span.x; i += 32) {
         const int64_t slot = (static_cast<int64_t>(span.x + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0);
@@ -702,32 +779,36 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     if ((tid & 31) == 0) lse2_sm[g] = lg;
   }
   __syncthreads();
-  const float* s = p.scores + (static_cast<int64_t>(b) * p.Hq + static_cast<int64_t>(hk) * p.G) * p.score_ld;
+  const float* s = p.scores + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld * p.score_heads;
   float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld;
   for (int64_t j = static_cast<int64_t>(share) * kJoinThreads + tid; j < L; j += static_cast<int64_t>(p.join_weight_ctas) * kJoinThreads) {
     float acc = 0.0f;
 #pragma unroll 4
-    for (int g = 0; g < p.G; ++g) acc += ex2(s[g * p.score_ld + j] - lse2_sm[g]);
+    for (int g = 0; g < p.G; g += 2) {
+      const float2 x = *reinterpret_cast<const float2*>(s + j * p.score_heads + g);
+      acc += ex2(x.x - lse2_sm[g]);
+      if (g + 1 < p.G) acc += ex2(x.y - lse2_sm[g + 1]);
+    }
     out[j] += acc;
   }
 }
 
 struct PagedPlan {
-  int groups, U, runs, part_rows;
-  int64_t score_ld;
+  int slots, groups, U, runs, part_rows, score_heads;
   size_t part, ml, tail, seq_runs, lse2, scores, bytes;     // offsets into the workspace
 };
 
-// (ctas_per_sm: 2 where the head dimension is not known; the workspace has room for that)
+// (ctas_per_sm: 4, the most of any kernel, where the head dimension is not known; the workspace has room for that)
 bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, PagedPlan* pl) {
   if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 8192 || B > (1 << 20) || Dv < 1 || Dv > 256 || ld < 0 || ld > 0x7FFFFFFF) return false;
   const int G = Hq / Hkv;
-  pl->groups = (G + kPRows - 1) / kPRows;
+  pl->slots = G <= 8 ? 8 : kMaxSlots;
+  pl->groups = (G + pl->slots - 1) / pl->slots;
   pl->U = Hkv * pl->groups;
   pl->runs = sm_count() * ctas_per_sm / pl->U;
   if (pl->runs < 1) pl->runs = 1;
-  pl->part_rows = G < kPRows ? G : kPRows;
-  pl->score_ld = (ld + 3) / 4 * 4;
+  pl->part_rows = G < pl->slots ? G : pl->slots;
+  pl->score_heads = (G + 1) / 2 * 2;
   const size_t ctas = static_cast<size_t>(pl->runs) * pl->U;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -740,15 +821,15 @@ bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, Pag
   pl->tail = take(ctas * sizeof(int2));
   pl->seq_runs = take(static_cast<size_t>(B) * sizeof(int2));
   pl->lse2 = take(static_cast<size_t>(B) * Hq * 4);
-  pl->scores = take(static_cast<size_t>(B) * Hq * pl->score_ld * 4);
+  pl->scores = take(static_cast<size_t>(B) * Hkv * ld * pl->score_heads * 4);
   pl->bytes = round_up(at, 1024);
   return true;
 }
 
-template <bool kInt8, int DP>
+template <bool kInt8, int DP, int kHeads>
 msd_status_t launch_paged(const PagedAttnParams& p, cudaStream_t s) {
-  using Sh = Shape<kInt8, DP>;
-  auto kernel = attn_paged_kernel<kInt8, DP>;
+  using Sh = Shape<kInt8, DP, kHeads>;
+  auto kernel = attn_paged_kernel<kInt8, DP, kHeads>;
   static DeviceOnce once;
   if (!once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem) == cudaSuccess; })) return MSD_ERR_CUDA;
   const bool pdl = option(OPT_NO_PDL) != 1;
@@ -765,6 +846,27 @@ msd_status_t launch_paged(const PagedAttnParams& p, cudaStream_t s) {
   return MSD_OK;
 }
 
+// f(kernel shape) for the shape of a call
+template <typename F>
+auto with_shape(bool int8, int widest, int slots, F&& f) {
+  auto heads = [&](auto i8, auto dp) {
+    return slots == 8 ? f.template operator()<decltype(i8)::value, decltype(dp)::value, 8>() : f.template operator()<decltype(i8)::value, decltype(dp)::value, 16>();
+  };
+  auto size = [&](auto i8) {
+    return widest <= 64 ? heads(i8, std::integral_constant<int, 64>{})
+                        : (widest <= 128 ? heads(i8, std::integral_constant<int, 128>{}) : heads(i8, std::integral_constant<int, 256>{}));
+  };
+  return int8 ? size(std::true_type{}) : size(std::false_type{});
+}
+struct CtasPerSm {
+  template <bool kInt8, int DP, int kHeads> int operator()() const { return Shape<kInt8, DP, kHeads>::kCtasPerSm; }
+};
+struct Launch {
+  const PagedAttnParams& p;
+  cudaStream_t s;
+  template <bool kInt8, int DP, int kHeads> msd_status_t operator()() const { return launch_paged<kInt8, DP, kHeads>(p, s); }
+};
+
 }  // namespace
 
 }  // namespace msd
@@ -773,7 +875,7 @@ extern "C" {
 
 size_t msd_attn_decode_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Dv, int64_t ld) {
   msd::PagedPlan pl;
-  return msd::plan_paged(B, Hq, Hkv, Dv, ld, 2, &pl) ? pl.bytes : 0;
+  return msd::plan_paged(B, Hq, Hkv, Dv, ld, 4, &pl) ? pl.bytes : 0;
 }
 
 msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_paged_cache_t* cache, const int32_t* block_table,
@@ -786,9 +888,9 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   if (q_ld < static_cast<int64_t>(Hq) * cache->D) return MSD_ERR_BAD_SHAPE;
   if (B == 0) return MSD_OK;
   const bool int8 = cache->type == MSD_CACHE_INT8;
-  const int widest = cache->D > cache->Dv ? cache->D : cache->Dv, dp = widest <= 64 ? 64 : (widest <= 128 ? 128 : 256);
+  const int widest = cache->D > cache->Dv ? cache->D : cache->Dv, slots = Hq / cache->Hkv <= 8 ? 8 : kMaxSlots;
   PagedPlan pl;
-  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, dp == 256 ? 1 : 2, &pl)) return MSD_ERR_UNSUPPORTED;
+  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, with_shape(int8, widest, slots, CtasPerSm{}), &pl)) return MSD_ERR_UNSUPPORTED;
   if (!q_bf16 || !block_table || !seqlens || !out_bf16 || !workspace) return MSD_ERR_NULL_POINTER;
   if (!aligned(q_bf16, 16) || q_ld % 8 != 0 || !aligned(out_bf16, 16) || !aligned(workspace, 1024) || !aligned(block_table, 4) ||
       !aligned(seqlens, 4) || !aligned(lse, 4) || !aligned(weights, 4))
@@ -817,7 +919,9 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.lse = lse;
   p.weights = weights;
   p.ld = ld;
-  p.score_ld = pl.score_ld;
+  p.score_ld = ld;
+  p.score_heads = pl.score_heads;
+  p.slots = pl.slots;
   p.part = reinterpret_cast<float*>(ws + pl.part);
   p.part_ml = reinterpret_cast<float*>(ws + pl.ml);
   p.tail = reinterpret_cast<int2*>(ws + pl.tail);
@@ -829,8 +933,7 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   const int64_t most = (ld + kJoinThreads - 1) / kJoinThreads, fill = (8LL * sm_count() + static_cast<int64_t>(B) * cache->Hkv - 1) / (static_cast<int64_t>(B) * cache->Hkv);
   p.join_weight_ctas = static_cast<int>(most < fill ? (most < 1 ? 1 : most) : fill);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (int8) return dp == 64 ? launch_paged<true, 64>(p, s) : (dp == 128 ? launch_paged<true, 128>(p, s) : launch_paged<true, 256>(p, s));
-  return dp == 64 ? launch_paged<false, 64>(p, s) : (dp == 128 ? launch_paged<false, 128>(p, s) : launch_paged<false, 256>(p, s));
+  return with_shape(int8, widest, slots, Launch{p, s});
 }
 
 }  // extern "C"

@@ -20,8 +20,8 @@ def _args(c):
 def _check_attention(q, c, scale, got, lse=None, before=None, weights=None):
     """What the arithmetic allows: a score is a sum of D products in FP32, then scaled (and for INT8 scaled again): off by at most
     d = (D + 8) 2^-23 sum |q k| scale; the softmax of scores that are off by d has probabilities off by a factor e^(2d), and exp2, the
-    sums and the division add a few FP32 roundings (16 are granted).  P (INT8: times the value's scale) is rounded to BF16 once,
-    the result once more."""
+    sums and the division add a few FP32 roundings (16 are granted).  P goes into the product as two BF16 values, which leave out
+    2^-16 of it (INT8: P times the value's scale, relative to the largest scale, as one FP16 value: 2^-11); the result is rounded to BF16."""
     want, want_lse, want_w, mass, reach = attention(q, c, scale)
     D = q.shape[2]
     d = (D + 8) * FP32 * reach
@@ -29,7 +29,8 @@ def _check_attention(q, c, scale, got, lse=None, before=None, weights=None):
     # sums over the tokens: FP32 additions in chains of at most (length / 64 + 64)
     longest = int(c["seqlens"].max()) if len(c["seqlens"]) else 0
     rel = rel + (longest / 64 + 64) * FP32
-    bound = HALF_BF16 * want.abs() + (HALF_BF16 + rel[..., None]) * mass * (1 + 2 * HALF_BF16)
+    p_rounding = 2.0 ** -16 if c["k_scale"] is None else 2.0 ** -11
+    bound = HALF_BF16 * want.abs() + (p_rounding + rel[..., None]) * mass * (1 + 2 * HALF_BF16)
     assert torch.isfinite(got.float()).all()
     assert ((got.double() - want).abs() <= bound + 1e-38).all(), ((got.double() - want).abs() - bound).max()
     if lse is not None:

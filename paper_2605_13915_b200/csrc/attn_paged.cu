@@ -37,6 +37,8 @@ constexpr int kJoinThreads = 256;
 
 struct PagedAttnParams {
   PagedCache c;
+  // strides of the cache between blocks and tokens: rows in units of 16 bytes, scales in words (offsets fit 32 bits)
+  uint32_t k_block, k_token, v_block, v_token, ks_block, ks_token, vs_block, vs_token;
   const uint16_t* q;
   int64_t q_ld;
   const int32_t* table;
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(kPThreads, (Shape<kInt8, DP, kHeads>::kCtasPer
 attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   using S = Shape<kInt8, DP, kHeads>;
   constexpr int NT = kHeads / 8;                        // column tiles of heads
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ int scan_buf[kPWarps];
   __shared__ int start_buf[2];
   __shared__ float ml[2][kPWarps][kHeads];
@@ -230,73 +232,80 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   ld.tiles = (ld.L + S::kTile - 1) / S::kTile;
   ld.left = end - first;
   Walk cur = ld;
-  auto advance = [&](Walk& w) {
-    --w.left;
-    if (++w.tile == w.tiles && w.left > 0) {
-      do {
-        w.L = seq_len(p, ++w.b);
-      } while (w.L == 0);
-      w.tile = 0;
-      w.tiles = (w.L + S::kTile - 1) / S::kTile;
-    }
+  auto next_sequence = [&](Walk& w) {
+    do {
+      w.L = seq_len(p, ++w.b);
+    } while (w.L == 0);
+    w.tile = 0;
+    w.tiles = (w.L + S::kTile - 1) / S::kTile;
   };
 
   // ---- loads ----
   uint8_t* ring = smem + warp * (S::kStages * S::kStage);
   const uint32_t ring_u = smem_u32(ring);
-  const uint8_t* kbase = p.c.k.base + hk * p.c.k.head;
-  const uint8_t* vbase = p.c.v.base + hk * p.c.v.head;
   constexpr int kChunks = S::kRow / 16;                 // 16-byte chunks of a row
   constexpr int kRowsPer = 32 / kChunks;                // rows that one instruction of the warp brings
-  const int k_chunks = p.c.D * S::kEs / 16, v_chunks = p.c.Dv * S::kEs / 16;
   const int my_chunk = lane % kChunks, my_row = lane / kChunks;
+  const uint8_t* kbase = p.c.k.base + hk * p.c.k.head + my_chunk * 16;
+  const uint8_t* vbase = p.c.v.base + hk * p.c.v.head + my_chunk * 16;
+  const uint8_t* ksbase = kInt8 ? p.c.ks.base + hk * p.c.ks.head : nullptr;
+  const uint8_t* vsbase = kInt8 ? p.c.vs.base + hk * p.c.vs.head : nullptr;
+  const bool k_there = my_chunk * 16 < p.c.D * S::kEs, v_there = my_chunk * 16 < p.c.Dv * S::kEs;
   const int tok_lane = lane & (S::kTok - 1);
-  // the block of this lane's token of the tile that `ld` stands on, asked for a tile ahead
-  auto look_up = [&](const Walk& w) -> int {
-    const int pos = w.tile * S::kTile + warp * S::kTok + tok_lane;
-    if (w.left <= 0 || pos >= w.L) return -1;
-    return p.table[static_cast<int64_t>(w.b) * p.max_blocks + div_by(pos, p.c.page)];
+  // The block of this lane's token of the tile that `ld` stands on, asked for a tile ahead; -1 behind the end.
+  const int32_t* ld_table = p.table + static_cast<int64_t>(ld.b) * p.max_blocks;
+  int ld_pos = ld.tile * S::kTile + warp * S::kTok + tok_lane;
+  uint32_t ld_page = 0;
+  int blk = -1;
+  auto look_up = [&]() {
+    blk = -1;
+    if (ld_pos < ld.L) {
+      ld_page = div_by(ld_pos, p.c.page);
+      blk = ld_table[ld_page];
+    }
   };
-  int blk = look_up(ld);
-  auto issue = [&](int stage) {
+  look_up();
+  auto issue = [&](uint32_t dst) {
     if (ld.left > 0) {
-      const int pos = ld.tile * S::kTile + warp * S::kTok + tok_lane;
-      bool there = pos < ld.L;
-      if (there && static_cast<uint32_t>(blk) >= static_cast<uint64_t>(p.c.num_blocks)) {
-        atomicMax(p.status, kStatusBadShape);
-        there = false;
-      }
-      const uint32_t slot = pos - div_by(pos, p.c.page) * p.c.page.d;
-      const int64_t ko = there ? row_offset(p.c.k, blk, slot) : -1, vo = there ? row_offset(p.c.v, blk, slot) : -1;
-      const uint32_t dst = ring_u + stage * S::kStage;
+      const bool wanted = ld_pos < ld.L;
+      const bool there = wanted && static_cast<uint32_t>(blk) < static_cast<uint32_t>(p.c.num_blocks);
+      if (wanted && !there) atomicMax(p.status, kStatusBadShape);
+      const uint32_t slot = ld_pos - ld_page * p.c.page.d, at = there ? blk : 0;
+      const uint32_t in = there ? slot : 0;
+      const uint32_t ko = at * p.k_block + in * p.k_token, vo = at * p.v_block + in * p.v_token;
+      const uint32_t mask = __ballot_sync(0xffffffffu, there) >> my_row;      // (lanes 16-31 repeat the tokens of a tile of 16)
+      const uint32_t k_mask = k_there ? mask : 0u, v_mask = v_there ? mask : 0u;
 #pragma unroll
       for (int i = 0; i < S::kTok / kRowsPer; ++i) {
         const int r = i * kRowsPer + my_row;
-        const int64_t o = __shfl_sync(0xffffffffu, ko, r);
-        const bool ok = o >= 0 && my_chunk < k_chunks;
-        cp16(dst + swz<S::kRow>(r, my_chunk), kbase + (ok ? o + my_chunk * 16 : 0), ok);
+        const uint32_t o = __shfl_sync(0xffffffffu, ko, r);
+        cp16(dst + swz<S::kRow>(r, my_chunk), kbase + static_cast<uint64_t>(o) * 16, (k_mask >> (i * kRowsPer)) & 1u);
       }
 #pragma unroll
       for (int i = 0; i < S::kTok / kRowsPer; ++i) {
         const int r = i * kRowsPer + my_row;
-        const int64_t o = __shfl_sync(0xffffffffu, vo, r);
-        const bool ok = o >= 0 && my_chunk < v_chunks;
-        cp16(dst + S::kHalf + swz<S::kRow>(r, my_chunk), vbase + (ok ? o + my_chunk * 16 : 0), ok);
+        const uint32_t o = __shfl_sync(0xffffffffu, vo, r);
+        cp16(dst + S::kHalf + swz<S::kRow>(r, my_chunk), vbase + static_cast<uint64_t>(o) * 16, (v_mask >> (i * kRowsPer)) & 1u);
       }
       if constexpr (kInt8) {
         const uint32_t sc = dst + 2 * S::kHalf + tok_lane * 4;
-        const int64_t kso = there ? row_offset(p.c.ks, blk, slot) + hk * p.c.ks.head : 0;
-        const int64_t vso = there ? row_offset(p.c.vs, blk, slot) + hk * p.c.vs.head : 0;
-        if (S::kTok == 32 || lane < 16) cp4(sc, p.c.ks.base + kso, there);
-        if (S::kTok == 32 || lane >= 16) cp4(sc + S::kScale, p.c.vs.base + vso, there);
+        const uint32_t kso = at * p.ks_block + in * p.ks_token, vso = at * p.vs_block + in * p.vs_token;
+        if (S::kTok == 32 || lane < 16) cp4(sc, ksbase + static_cast<uint64_t>(kso) * 4, there);
+        if (S::kTok == 32 || lane >= 16) cp4(sc + S::kScale, vsbase + static_cast<uint64_t>(vso) * 4, there);
       }
-      advance(ld);
-      blk = look_up(ld);
+      --ld.left;
+      ld_pos += S::kTile;
+      if (++ld.tile == ld.tiles && ld.left > 0) {
+        next_sequence(ld);
+        ld_table = p.table + static_cast<int64_t>(ld.b) * p.max_blocks;
+        ld_pos = warp * S::kTok + tok_lane;
+      }
+      look_up();
     }
     cp_commit();
   };
 #pragma unroll
-  for (int s = 0; s < S::kStages - 1; ++s) issue(s);
+  for (int s = 0; s < S::kStages - 1; ++s) issue(ring_u + s * S::kStage);
 
   // ---- the arithmetic ----
   const int row = lane >> 2, quad = lane & 3;           // a thread has tokens (or values of d) `row`, `row` + 8 and heads 2 quad, 2 quad + 1
@@ -379,7 +388,14 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) f[n][0] = f[n][1] = p.scale2;
 
-  int it = 0;
+  // Matrices of the fragments: token (lane & 15) of 16, chunks c and c + 1 by the upper half of the warp; BF16 values: tokens by the upper
+  // half, chunks by the eighths.  The swizzle moves only the lowest three bits of a chunk's number (two where a row is 64 bytes), so
+  // chunk c is an exclusive or away from chunk 0, and what lies above those bits an offset.
+  const uint32_t k_lane = swz<S::kRow>(lane & 15, lane >> 4);
+  const uint32_t v_lane = S::kHalf + (kInt8 ? k_lane : swz<S::kRow>(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
+  constexpr int kSwz = S::kRow >= 128 ? 7 : 3;
+  uint32_t stage_u = ring_u, fill_u = ring_u + (S::kStages - 1) * S::kStage;      // the stage of this tile, and the one to fill
+  const float* stage_scales = reinterpret_cast<const float*>(ring + 2 * S::kHalf);
   while (cur.left > 0) {
     // a segment: the tiles of one sequence that are in this run
     const int seg_first = cur.tile;
@@ -396,16 +412,24 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     // INT8: a power of two that no value's scale so far exceeds (2^-111 at least, so that 2^15 / vref is finite); outputs are in units of vref / 2^15
     float vref = 3.851859888774472e-34f;
 
-    for (int t = 0; t < seg; ++t, ++it) {
-      const int stage = it % S::kStages;
+    float* score_at = nullptr;
+    if (p.weights)
+      score_at = p.scores + ((static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + warp * S::kTok + row) * p.score_heads + h0 + 2 * quad;
+    for (int t = 0; t < seg; ++t) {
       cp_wait<S::kStages - 2>();
       __syncwarp();
-      issue((it + S::kStages - 1) % S::kStages);        // the stage that the last tile left
-      const int pos0 = cur.tile * S::kTile + warp * S::kTok;
-      advance(cur);
+      issue(fill_u);                                    // the stage that the last tile left
+      const uint32_t k_u = stage_u + k_lane, v_u = stage_u + v_lane;
+      const float* scales = stage_scales;
+      fill_u = stage_u;
+      stage_u += S::kStage;
+      stage_scales += S::kStage / 4;
+      if (stage_u == ring_u + S::kStages * S::kStage) {
+        stage_u = ring_u;
+        stage_scales -= S::kStages * S::kStage / 4;
+      }
+      const int tile = seg_first + t, pos0 = tile * S::kTile + warp * S::kTok;
       if (pos0 >= L) continue;                          // (uniform in the warp)
-      const uint32_t sk = ring_u + stage * S::kStage, sv = sk + S::kHalf;
-      const float* scales = reinterpret_cast<const float*>(ring + stage * S::kStage + 2 * S::kHalf);
       constexpr int kGroups = S::kTok / 16;
 
       // scores of 16 tokens (rows) and 8 heads (columns) a fragment
@@ -415,10 +439,13 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[g][n][0] = s[g][n][1] = s[g][n][2] = s[g][n][3] = 0.0f;
 #pragma unroll
-        for (int c = 0; c < kSteps; c += kInt8 ? 2 : 1) {
-          if (c < k_steps) {
+        for (int c4 = 0; c4 < kSteps; c4 += 4) {        // 64 values of d at a time: what is past D is zero in both
+          if (c4 >= k_steps) break;
+#pragma unroll
+          for (int c = c4; c < c4 + 4; c += kInt8 ? 2 : 1) {
             uint32_t r[4];
-            ldsm4(r, sk + swz<S::kRow>(g * 16 + (lane & 15), (kInt8 ? c : 2 * c) + (lane >> 4)));
+            const int chunk = kInt8 ? c : 2 * c;
+            ldsm4(r, (k_u ^ ((chunk & kSwz) << 4)) + ((chunk & ~kSwz) << 4) + g * 16 * S::kRow);
             if constexpr (kInt8) {                      // a register: four codes of a token; two registers a step
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
@@ -451,7 +478,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
           }
         }
         if (p.weights) {
-          float* dst = p.scores + ((static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + pos0 + g * 16 + row) * p.score_heads + h0 + 2 * quad;
+          float* dst = score_at + static_cast<int64_t>(tile * S::kTile + g * 16) * p.score_heads;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             if (n * 8 + 2 * quad < nh) {
@@ -541,11 +568,14 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
-        for (int c = 0; c < DP / 16; c += kInt8 ? 2 : 1) {
-          if (c < v_steps) {
+        for (int c4 = 0; c4 < DP / 16; c4 += 4) {
+          if (c4 >= v_steps) break;
+#pragma unroll
+          for (int c = c4; c < c4 + 4; c += kInt8 ? 2 : 1) {
             uint32_t r[4];
+            const int chunk = kInt8 ? c : 2 * c;
+            ldsm4_t(r, (v_u ^ ((chunk & kSwz) << 4)) + ((chunk & ~kSwz) << 4) + g * 16 * S::kRow);
             if constexpr (kInt8) {                      // a register: two tokens of an even and the next odd value of d
-              ldsm4_t(r, sv + swz<S::kRow>(g * 16 + (lane & 15), c + (lane >> 4)));
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
                 const uint32_t x = r[2 * j] ^ 0x80808080u, y = r[2 * j + 1] ^ 0x80808080u;
@@ -554,7 +584,6 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
                 for (int n = 0; n < NT; ++n) mma16<true>(o[n][c + j], a, ph[g][n]);
               }
             } else {
-              ldsm4_t(r, sv + swz<S::kRow>(g * 16 + ((lane >> 4) << 3) + (lane & 7), 2 * c + ((lane >> 3) & 1)));
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 mma16<false>(o[n][c], r, ph[g][n]);
@@ -565,6 +594,8 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         }
       }
     }
+    cur.left -= seg;
+    if (cur.left > 0) next_sequence(cur);               // (a segment that is not the run's last one ends its sequence)
 
     // ---- the segment's end: the warps meet ----
 #pragma unroll
@@ -781,15 +812,35 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
   __syncthreads();
   const float* s = p.scores + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld * p.score_heads;
   float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld;
-  for (int64_t j = static_cast<int64_t>(share) * kJoinThreads + tid; j < L; j += static_cast<int64_t>(p.join_weight_ctas) * kJoinThreads) {
-    float acc = 0.0f;
-#pragma unroll 4
-    for (int g = 0; g < p.G; g += 2) {
-      const float2 x = *reinterpret_cast<const float2*>(s + j * p.score_heads + g);
-      acc += ex2(x.x - lse2_sm[g]);
-      if (g + 1 < p.G) acc += ex2(x.y - lse2_sm[g + 1]);
+  constexpr int kAtOnce = 4;                     // positions of a thread whose loads are under way together
+  const int step = p.join_weight_ctas * kJoinThreads;
+  for (int64_t j0 = static_cast<int64_t>(share) * kJoinThreads + tid; j0 < L; j0 += static_cast<int64_t>(step) * kAtOnce) {
+    float acc[kAtOnce], was[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      acc[i] = 0.0f;
+      const int64_t j = j0 + static_cast<int64_t>(i) * step;
+      was[i] = j < L ? out[j] : 0.0f;
     }
-    out[j] += acc;
+    for (int g = 0; g < p.G; g += 2) {
+      const float l0 = lse2_sm[g], l1 = g + 1 < p.G ? lse2_sm[g + 1] : INFINITY;      // (no weight for a head that is not there)
+      float2 x[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int64_t j = j0 + static_cast<int64_t>(i) * step;
+        x[i] = j < L ? __ldcs(reinterpret_cast<const float2*>(s + j * p.score_heads + g)) : make_float2(0.0f, 0.0f);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        acc[i] += ex2(x[i].x - l0);
+        if (l1 != INFINITY) acc[i] += ex2(x[i].y - l1);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int64_t j = j0 + static_cast<int64_t>(i) * step;
+      if (j < L) out[j] = was[i] + acc[i];
+    }
   }
 }
 
@@ -896,6 +947,18 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
       !aligned(seqlens, 4) || !aligned(lse, 4) || !aligned(weights, 4))
     return MSD_ERR_BAD_ALIGNMENT;
   if (workspace_bytes < pl.bytes) return MSD_ERR_WORKSPACE_TOO_SMALL;
+  const int64_t page = cache->page_size, blocks = cache->num_blocks, most_rows = int64_t{1} << 36, most_scales = int64_t{1} << 34;
+  if (!rows_within(p.c.k, blocks, page, most_rows) || !rows_within(p.c.v, blocks, page, most_rows) ||
+      (int8 && !(rows_within(p.c.ks, blocks, page, most_scales) && rows_within(p.c.vs, blocks, page, most_scales))))
+    return MSD_ERR_UNSUPPORTED;
+  p.k_block = static_cast<uint32_t>(p.c.k.block / 16);
+  p.k_token = static_cast<uint32_t>(p.c.k.token / 16);
+  p.v_block = static_cast<uint32_t>(p.c.v.block / 16);
+  p.v_token = static_cast<uint32_t>(p.c.v.token / 16);
+  p.ks_block = static_cast<uint32_t>(p.c.ks.block / 4);
+  p.ks_token = static_cast<uint32_t>(p.c.ks.token / 4);
+  p.vs_block = static_cast<uint32_t>(p.c.vs.block / 4);
+  p.vs_token = static_cast<uint32_t>(p.c.vs.token / 4);
   p.status = device_status_ptr();
   if (!p.status) return MSD_ERR_CUDA;
   uint8_t* ws = static_cast<uint8_t*>(workspace);

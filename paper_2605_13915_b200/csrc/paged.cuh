@@ -32,6 +32,11 @@ struct PagedCache {
   int Hkv, D, Dv;
 };
 
+// Whether the rows of a head start less than `most` bytes from one another.
+inline bool rows_within(const PagedRows& r, int64_t blocks, int64_t page, int64_t most) {
+  return static_cast<__int128>(blocks - 1) * r.block + static_cast<__int128>(page - 1) * r.token < most;
+}
+
 __device__ __forceinline__ int64_t row_offset(const PagedRows& r, int32_t blk, uint32_t slot) { return blk * r.block + slot * r.token; }
 
 // Fills in the device's view; MSD_OK or why the cache is refused.

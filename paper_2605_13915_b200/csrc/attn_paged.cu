@@ -34,6 +34,8 @@ constexpr int kPWarps = 4;
 constexpr int kPThreads = 32 * kPWarps;
 constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
+constexpr float kHeld = 8.0f;               // how far (log2) a score may exceed its reference before that moves
+constexpr float kPUnits = 128.0f;           // INT8: 2^15 / 2^kHeld
 
 struct PagedAttnParams {
   PagedCache c;
@@ -122,20 +124,24 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
 template <bool kInt8, int DP, int kHeads>
 struct Shape {
   static constexpr int kEs = kInt8 ? 1 : 2;
-  static constexpr int kTok = kInt8 && DP == 64 ? 32 : 16;
+  static constexpr int kTok = kInt8 && DP <= 128 ? 32 : 16;
   static constexpr int kRow = DP * kEs;                         // bytes of a row in shared memory
   static constexpr int kHalf = kTok * kRow;                     // keys, then values
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
-  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kHalf >= 4096 ? 2 : (kHeads == 8 ? 4 : 3));
-  static constexpr int kStages = kHeads == 16 && kHalf <= 2048 ? 4 : (kHeads == 16 && kInt8 && DP == 256 ? 2 : 3);
+  static constexpr bool kWide = kHalf >= 4096;                  // 8 KB a tile and more
+  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (kInt8 && DP == 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
+  static constexpr int kStages = kWide ? (kCtasPerSm == 3 ? 2 : 3) : (kHeads == 8 ? 3 : 4);
   static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
   static constexpr int kRing = kPWarps * kStages * kStage;
-  static constexpr int kORow = DP + 4;
-  static constexpr int kOut = kHeads * kORow * 4;               // where the warps' outputs meet
-  static constexpr int kSmem = kRing + kOut + (kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0);
+  // The warps' outputs meet in the stages that their last tiles left, all heads or 8 at a time; rows four words apart in the banks
+  // where there is room for that.
+  static constexpr int kMeet = kHeads * DP * 4 <= kStage ? kHeads : 8;
+  static constexpr int kORow = kMeet * (DP + 4) * 4 <= kStage ? DP + 4 : DP;
+  static constexpr int kSmem = kRing + (kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0);
   static constexpr int kTile = kPWarps * kTok;                  // tokens of a CTA's tile
-  static_assert(kCtasPerSm * (kSmem + 1600) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
+  static_assert(kMeet * kORow * 4 <= kStage, "a stage has to hold a warp's outputs");
+  static_assert(kCtasPerSm * (kSmem + 2304) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
 };
 
 // 16-byte chunk c of row r, so that the eight rows of a matrix lie in different banks
@@ -155,9 +161,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   using S = Shape<kInt8, DP, kHeads>;
   constexpr int NT = kHeads / 8;                        // column tiles of heads
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ int scan_buf[kPWarps];
-  __shared__ int start_buf[2];
-  __shared__ float ml[2][kPWarps][kHeads];
+  __shared__ float ml[3][kPWarps][kHeads];              // of a warp: references, sums, units of its outputs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
   const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kHeads;        // first head of the group within the KV head
@@ -167,67 +171,57 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   pdl_wait_primary();
   pdl_launch_dependents();
 
-  // ---- this CTA's run of tiles ----
-  const int b_first = threadIdx.x;
-  int total = 0, tiles_first = 0;
-  for (int b = b_first; b < p.B; b += kPThreads) {
+  // ---- this CTA's run of tiles ----  (every warp by itself; a lane looks at a share of the sequences)
+  const int per_lane = (p.B + 31) / 32, b_lo = min(p.B, lane * per_lane), b_hi = min(p.B, b_lo + per_lane);
+  int mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
     const int32_t n = p.seqlens[b];
-    const int L = seq_len(p, b);
-    if (L != n && unit == 0 && run == 0) atomicMax(p.status, kStatusBadShape);
-    const int t = (L + S::kTile - 1) / S::kTile;
-    if (b == b_first) tiles_first = t;
-    total += t;
-    if (L == 0 && b % p.runs == run) {           // nothing to attend to
-      for (int h = 0; h < nh; ++h) {
-        const int64_t row = static_cast<int64_t>(b) * p.Hq + head0 + h;
-        for (int d = 0; d < p.c.Dv; d += 8) *reinterpret_cast<uint4*>(p.out + row * p.c.Dv + d) = make_uint4(0, 0, 0, 0);
-        if (p.lse) p.lse[row] = -INFINITY;
+    const int L = static_cast<int>(min(static_cast<int64_t>(max(n, 0)), p.cap));
+    if (warp == 0) {
+      if (L != n && blockIdx.x == 0) atomicMax(p.status, kStatusBadShape);
+      if (L == 0 && b % p.runs == run) {         // nothing to attend to
+        for (int h = 0; h < nh; ++h) {
+          const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + h;
+          for (int d = 0; d < p.c.Dv; d += 8) *reinterpret_cast<uint4*>(p.out + out_row * p.c.Dv + d) = make_uint4(0, 0, 0, 0);
+          if (p.lse) p.lse[out_row] = -INFINITY;
+        }
       }
     }
+    mine += (L + S::kTile - 1) / S::kTile;
   }
-  auto block_scan = [&](int v, int* sum) {       // inclusive, over the threads of the block
-    int x = v;
+  int before = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    __syncthreads();
-    if (lane == 31) scan_buf[warp] = x;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < kPWarps; ++w) {
-      if (w < warp) x += scan_buf[w];
-      all += scan_buf[w];
-    }
-    *sum = all;
-    return x;
-  };
-  int T;
-  block_scan(total, &T);
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, before, d);
+    if (lane >= d) before += y;
+  }
+  const int T = __shfl_sync(0xffffffffu, before, 31);
+  before -= mine;
   if (threadIdx.x == 0) p.tail[blockIdx.x] = make_int2(-1, 0);
   const int runs = min(p.runs, T);                // (no empty runs)
   if (run >= runs) return;
   auto run_start = [&](int r) { return static_cast<int>(static_cast<int64_t>(r) * T / runs); };
   const int first = run_start(run), end = run_start(run + 1);
-  for (int base = 0, carry = 0; base < p.B && carry <= first; base += kPThreads) {
-    const int b = base + threadIdx.x;
-    const int t = base == 0 ? tiles_first : (b < p.B ? (seq_len(p, b) + S::kTile - 1) / S::kTile : 0);
-    int sum;
-    const int incl = carry + block_scan(t, &sum);
-    if (first >= incl - t && first < incl) { start_buf[0] = b; start_buf[1] = first - (incl - t); }
-    carry += sum;
+  const bool here = first >= before && first < before + mine;       // of one lane
+  int b_first = b_lo, t_first = first - before;
+  if (here) {
+    for (;; ++b_first) {
+      const int t = (seq_len(p, b_first) + S::kTile - 1) / S::kTile;
+      if (t_first < t) break;
+      t_first -= t;
+    }
   }
-  __syncthreads();
+  const int owner = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+  b_first = __shfl_sync(0xffffffffu, b_first, owner);
+  t_first = __shfl_sync(0xffffffffu, t_first, owner);
 
   // A walk over the tiles of the run, one for the loads and one for the arithmetic.
   struct Walk {
     int b, tile, tiles, L, left;          // sequence, tile of it, tiles of it, its length, tiles left in the run
   };
   Walk ld;
-  ld.b = start_buf[0];
-  ld.tile = start_buf[1];
+  ld.b = b_first;
+  ld.tile = t_first;
   ld.L = seq_len(p, ld.b);
   ld.tiles = (ld.L + S::kTile - 1) / S::kTile;
   ld.left = end - first;
@@ -309,8 +303,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 
   // ---- the arithmetic ----
   const int row = lane >> 2, quad = lane & 3;           // a thread has tokens (or values of d) `row`, `row` + 8 and heads 2 quad, 2 quad + 1
-  float* sm_o = reinterpret_cast<float*>(smem + S::kRing);
-  uint2* sm_q = reinterpret_cast<uint2*>(smem + S::kRing + S::kOut);
+  uint2* sm_q = reinterpret_cast<uint2*>(smem + S::kRing);
   constexpr int kSteps = DP / 16;
   uint2 qf[S::kQInSmem ? 1 : kSteps][NT];
   float o[NT][DP / 16][4];
@@ -320,22 +313,31 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   // The query as column fragments: head `row` of each tile.  INT8: of 16 values of d a thread's bytes are 4 quad ... 4 quad + 3, so the
   // query is taken in that order too, and goes into FP16 scaled by a power of two that brings its largest value to 2^14 ... 2^15: what
   // is 2^-29 of that or more stays exact, the rest is off by 2^-40 of it at most.
-  auto load_q = [&]() {
+  auto raw_q = [&](int s, int n) {
     const uint16_t* q = p.q + static_cast<int64_t>(cur.b) * p.q_ld + head0 * p.c.D;
-    auto raw = [&](int s, int n) {
-      uint2 v = make_uint2(0, 0);
-      const int h = n * 8 + row;
-      const uint16_t* at = q + h * p.c.D + s * 16;
-      if (h < nh) {
-        if constexpr (kInt8) {
-          if (s * 16 + 4 * quad < p.c.D) v = *reinterpret_cast<const uint2*>(at + 4 * quad);
-        } else {
-          if (s * 16 + 2 * quad < p.c.D) v.x = *reinterpret_cast<const uint32_t*>(at + 2 * quad);
-          if (s * 16 + 2 * quad + 8 < p.c.D) v.y = *reinterpret_cast<const uint32_t*>(at + 2 * quad + 8);
-        }
+    uint2 v = make_uint2(0, 0);
+    const int h = n * 8 + row;
+    const uint16_t* at = q + h * p.c.D + s * 16;
+    if (h < nh) {
+      if constexpr (kInt8) {
+        if (s * 16 + 4 * quad < p.c.D) v = *reinterpret_cast<const uint2*>(at + 4 * quad);
+      } else {
+        if (s * 16 + 2 * quad < p.c.D) v.x = *reinterpret_cast<const uint32_t*>(at + 2 * quad);
+        if (s * 16 + 2 * quad + 8 < p.c.D) v.y = *reinterpret_cast<const uint32_t*>(at + 2 * quad + 8);
       }
-      return v;
-    };
+    }
+    return v;
+  };
+  auto fetch_q = [&]() {       // (of the sequence that `cur` stands on)
+    if constexpr (!S::kQInSmem) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) qf[s][n] = raw_q(s, n);
+      }
+    }
+  };
+  auto ready_q = [&]() {
     float up[NT];
     if constexpr (kInt8) {
 #pragma unroll
@@ -343,8 +345,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         uint32_t big = 0;                               // of |x| as BF16 bits, which grow with the value
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          const uint2 v = raw(s, n);
-          if constexpr (!S::kQInSmem) qf[s][n] = v;
+          const uint2 v = S::kQInSmem ? raw_q(s, n) : qf[S::kQInSmem ? 0 : s][n];
           big = __vmaxu2(big, __vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu));
         }
         big = max(big & 0xFFFFu, big >> 16);
@@ -370,14 +371,14 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     if constexpr (S::kQInSmem) {
       for (int s = warp; s < kSteps; s += kPWarps) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) sm_q[(s * NT + n) * 32 + lane] = fragment(raw(s, n), n);
+        for (int n = 0; n < NT; ++n) sm_q[(s * NT + n) * 32 + lane] = fragment(raw_q(s, n), n);
       }
       __syncthreads();
-    } else {
+    } else if constexpr (kInt8) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) qf[s][n] = fragment(kInt8 ? qf[s][n] : raw(s, n), n);
+        for (int s = 0; s < kSteps; ++s) qf[s][n] = fragment(qf[s][n], n);
       }
     }
   };
@@ -396,12 +397,13 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   constexpr int kSwz = S::kRow >= 128 ? 7 : 3;
   uint32_t stage_u = ring_u, fill_u = ring_u + (S::kStages - 1) * S::kStage;      // the stage of this tile, and the one to fill
   const float* stage_scales = reinterpret_cast<const float*>(ring + 2 * S::kHalf);
+  fetch_q();
   while (cur.left > 0) {
     // a segment: the tiles of one sequence that are in this run
     const int seg_first = cur.tile;
     const int seg = min(cur.tiles - cur.tile, cur.left);
     const int b = cur.b, L = cur.L;
-    load_q();
+    ready_q();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       m[n][0] = m[n][1] = -INFINITY;
@@ -409,8 +411,9 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
       for (int i = 0; i < DP / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
-    // INT8: a power of two that no value's scale so far exceeds (2^-111 at least, so that 2^15 / vref is finite); outputs are in units of vref / 2^15
-    float vref = 3.851859888774472e-34f;
+    // INT8: vref, a power of two that no value's scale so far exceeds (2^-111 at least, so that vinv is finite).  P times the scale is in
+    // units of vref / 2^7: at most 2^15 in FP16, 11 bits down to 2^-21 vref, off by 2^-32 vref below that.
+    float vref = 3.851859888774472e-34f, vinv = kPUnits / vref;
 
     float* score_at = nullptr;
     if (p.weights)
@@ -489,7 +492,8 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         }
       }
 
-      // softmax; the maximum of a head moves rarely, and only then do the lanes ask each other
+      // Softmax.  The reference of a head moves only when a score exceeds it by more than 2^8 (it cancels in the end; probabilities up to
+      // 2^8 cost nothing in FP32), which after the first tile is rare, and only then do the lanes ask each other for the maximum.
       float mx[NT][2];
       bool moved = false;
 #pragma unroll
@@ -499,7 +503,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
           mx[n][e] = fmaxf(s[0][n][e], s[0][n][2 + e]);
 #pragma unroll
           for (int g = 1; g < kGroups; ++g) mx[n][e] = fmaxf(mx[n][e], fmaxf(s[g][n][e], s[g][n][2 + e]));
-          moved = moved || mx[n][e] > m[n][e];
+          moved = moved || mx[n][e] > m[n][e] + kHeld;
         }
       }
       float vs[kGroups][2];
@@ -530,14 +534,16 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
             }
           }
         }
-        vref = vnew;
+        if constexpr (kInt8) {
+          vref = vnew;
+          vinv = kPUnits / vnew;
+        }
       }
       if constexpr (kInt8) {
-        const float c = 32768.0f / vref;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-          vs[g][0] = scales[S::kTok + g * 16 + row] * c;
-          vs[g][1] = scales[S::kTok + g * 16 + row + 8] * c;
+          vs[g][0] = scales[S::kTok + g * 16 + row] * vinv;
+          vs[g][1] = scales[S::kTok + g * 16 + row + 8] * vinv;
         }
       }
       // Probabilities as column fragments of the product with v: the transposes of the score fragments.  INT8: times the value's scale,
@@ -595,7 +601,10 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       }
     }
     cur.left -= seg;
-    if (cur.left > 0) next_sequence(cur);               // (a segment that is not the run's last one ends its sequence)
+    if (cur.left > 0) {                                 // (a segment that is not the run's last one ends its sequence)
+      next_sequence(cur);
+      fetch_q();
+    }
 
     // ---- the segment's end: the warps meet ----
 #pragma unroll
@@ -605,100 +614,85 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
         if (row == 0) {
-          ml[0][warp][n * 8 + 2 * quad + e] = m[n][e];
-          ml[1][warp][n * 8 + 2 * quad + e] = l[n][e];
+          const int h = n * 8 + 2 * quad + e;
+          ml[0][warp][h] = m[n][e];
+          ml[1][warp][h] = l[n][e];
+          if constexpr (kInt8) ml[2][warp][h] = vref * (1.0f / kPUnits);
         }
       }
     }
-    __syncthreads();
-    auto joined = [&](int h, float* mh, float* lh) {
-      float mm = ml[0][0][h];
+    const bool from_start = seg_first == 0, to_end = seg_first + seg == (L + S::kTile - 1) / S::kTile;
+    const int Dv = p.c.Dv, vecs = Dv / 4;
+    const int64_t slot = static_cast<int64_t>(blockIdx.x) * 2 + (from_start ? 1 : 0);
+    float* meet = reinterpret_cast<float*>(smem + (fill_u - smem_u32(smem)));      // this warp's stage; the others' are as far from their rings
 #pragma unroll
-      for (int w = 1; w < kPWarps; ++w) mm = fmaxf(mm, ml[0][w][h]);
-      float ll = 0.0f;
+    for (int pass = 0; pass < kHeads / S::kMeet; ++pass) {
 #pragma unroll
-      for (int w = 0; w < kPWarps; ++w) ll += ml[1][w][h] * (ml[0][w][h] == -INFINITY ? 0.0f : ex2(ml[0][w][h] - mm));
-      *mh = mm;
-      *lh = ll;
-    };
-    float out_f[NT][2];
+      for (int n = pass * (S::kMeet / 8); n < (pass + 1) * (S::kMeet / 8); ++n) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+        for (int e = 0; e < 2; ++e) {
+          if (n * 8 + 2 * quad + e < nh) {
+            float* dst = meet + (n * 8 + 2 * quad + e - pass * S::kMeet) * S::kORow;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float mh, lh;
-        joined(n * 8 + 2 * quad + e, &mh, &lh);
-        out_f[n][e] = m[n][e] == -INFINITY ? 0.0f : ex2(m[n][e] - mh) * (kInt8 ? vref * 3.0517578125e-05f : 1.0f);
-      }
-    }
-    constexpr int kORow = S::kORow;
-    for (int w = 0; w < kPWarps; ++w) {          // one after the other: the order of the sums is fixed
-      if (w == warp) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (n * 8 + 2 * quad + e < nh) {
-              float* dst = sm_o + (n * 8 + 2 * quad + e) * kORow;
-#pragma unroll
-              for (int i = 0; i < DP / 16; ++i) {
-                const float x = o[n][i][e] * out_f[n][e], y = o[n][i][2 + e] * out_f[n][e];
-                if constexpr (kInt8) {
-                  float2* at = reinterpret_cast<float2*>(dst + i * 16 + 2 * row);
-                  const float2 was = w > 0 ? *at : make_float2(0.0f, 0.0f);
-                  *at = make_float2(was.x + x, was.y + y);
-                } else {
-                  float* at = dst + i * 16 + row;
-                  at[0] = (w > 0 ? at[0] : 0.0f) + x;
-                  at[8] = (w > 0 ? at[8] : 0.0f) + y;
-                }
+            for (int i = 0; i < DP / 16; ++i) {
+              if constexpr (kInt8) {
+                *reinterpret_cast<float2*>(dst + i * 16 + 2 * row) = make_float2(o[n][i][e], o[n][i][2 + e]);
+              } else {
+                dst[i * 16 + row] = o[n][i][e];
+                dst[i * 16 + row + 8] = o[n][i][2 + e];
               }
             }
           }
         }
       }
       __syncthreads();
+      const float* met = reinterpret_cast<const float*>(smem + (fill_u - ring_u));      // warp 0's; the next one's is a ring further
+      const int heads = min(nh - pass * S::kMeet, S::kMeet);
+      for (int i = threadIdx.x; i < heads * vecs; i += kPThreads) {
+        const int hl = i / vecs, d = (i - hl * vecs) * 4, h = pass * S::kMeet + hl;
+        float mh = ml[0][0][h];
+#pragma unroll
+        for (int w = 1; w < kPWarps; ++w) mh = fmaxf(mh, ml[0][w][h]);
+        float lh = 0.0f;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kPWarps; ++w) {              // (a fixed order)
+          const float mw = ml[0][w][h];
+          if (mw != -INFINITY) {
+            const float r = ex2(mw - mh), u = kInt8 ? r * ml[2][w][h] : r;
+            const float4 x = *reinterpret_cast<const float4*>(met + w * (S::kStages * S::kStage / 4) + hl * S::kORow + d);
+            lh = fmaf(ml[1][w][h], r, lh);
+            v.x = fmaf(x.x, u, v.x);
+            v.y = fmaf(x.y, u, v.y);
+            v.z = fmaf(x.z, u, v.z);
+            v.w = fmaf(x.w, u, v.w);
+          }
+        }
+        if (from_start && to_end) {
+          const float inv = 1.0f / lh;
+          const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + h;
+          *reinterpret_cast<uint2*>(p.out + out_row * Dv + d) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+          if (d == 0) {
+            const float lg = mh + log2f(lh);
+            if (p.lse) p.lse[out_row] = lg * 0.6931471805599453f;
+            if (p.weights) p.lse2[out_row] = lg;
+          }
+        } else {
+          *reinterpret_cast<float4*>(p.part + (slot * p.part_rows + h) * Dv + d) = v;
+          if (d == 0) *reinterpret_cast<float2*>(p.part_ml + (slot * p.part_rows + h) * 2) = make_float2(mh, lh);
+        }
+      }
+      __syncthreads();
     }
-    const bool from_start = seg_first == 0, to_end = seg_first + seg == (L + S::kTile - 1) / S::kTile;
-    const int Dv = p.c.Dv, vecs = Dv / 4;
     if (from_start && unit == 0 && threadIdx.x == 0) {
       const int64_t at = first + (static_cast<int64_t>(end - first) - cur.left - seg);      // the sequence's first tile in the list
       const int64_t last = at + (L + S::kTile - 1) / S::kTile - 1;
       p.seq_runs[b] = make_int2(run, static_cast<int>(((last + 1) * runs - 1) / T));
     }
-    if (from_start && to_end) {
-      for (int i = threadIdx.x; i < nh * vecs; i += kPThreads) {
-        const int r = i / vecs, d = (i - r * vecs) * 4;
-        float mh, lh;
-        joined(r, &mh, &lh);
-        const float inv = 1.0f / lh;
-        const float4 v = *reinterpret_cast<const float4*>(sm_o + r * kORow + d);
-        const uint2 w = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
-        const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + r;
-        *reinterpret_cast<uint2*>(p.out + out_row * Dv + d) = w;
-        if (d == 0) {
-          const float lg = mh + log2f(lh);
-          if (p.lse) p.lse[out_row] = lg * 0.6931471805599453f;
-          if (p.weights) p.lse2[out_row] = lg;
-        }
-      }
-    } else {
-      const int64_t slot = static_cast<int64_t>(blockIdx.x) * 2 + (from_start ? 1 : 0);
-      for (int i = threadIdx.x; i < nh * vecs; i += kPThreads) {
-        const int r = i / vecs, d = (i - r * vecs) * 4;
-        *reinterpret_cast<float4*>(p.part + (slot * p.part_rows + r) * Dv + d) = *reinterpret_cast<const float4*>(sm_o + r * kORow + d);
-        if (d == 0) {
-          float mh, lh;
-          joined(r, &mh, &lh);
-          *reinterpret_cast<float2*>(p.part_ml + (slot * p.part_rows + r) * 2) = make_float2(mh, lh);
-        }
-      }
-      if (from_start && threadIdx.x == 0) {
-        const int64_t last = static_cast<int64_t>(end) + (L + S::kTile - 1) / S::kTile - seg - 1;
-        p.tail[blockIdx.x] = make_int2(b, static_cast<int>(((last + 1) * runs - 1) / T));
-      }
+    if (from_start && !to_end && threadIdx.x == 0) {
+      const int64_t last = static_cast<int64_t>(end) + (L + S::kTile - 1) / S::kTile - seg - 1;
+      p.tail[blockIdx.x] = make_int2(b, static_cast<int>(((last + 1) * runs - 1) / T));
     }
-    __syncthreads();
   }
   cp_wait<0>();
 }
@@ -810,37 +804,43 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     if ((tid & 31) == 0) lse2_sm[g] = lg;
   }
   __syncthreads();
-  const float* s = p.scores + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld * p.score_heads;
-  float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld;
   constexpr int kAtOnce = 4;                     // positions of a thread whose loads are under way together
-  const int step = p.join_weight_ctas * kJoinThreads;
-  for (int64_t j0 = static_cast<int64_t>(share) * kJoinThreads + tid; j0 < L; j0 += static_cast<int64_t>(step) * kAtOnce) {
+  const int step = p.join_weight_ctas * kJoinThreads, first = share * kJoinThreads + tid;
+  const int64_t score_step = static_cast<int64_t>(step) * p.score_heads;
+  const float* s = p.scores + ((static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + first) * p.score_heads;
+  float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld + first;
+  for (int left = L - first; left > 0; left -= step * kAtOnce, s += score_step * kAtOnce, out += static_cast<int64_t>(step) * kAtOnce) {
     float acc[kAtOnce], was[kAtOnce];
+    const int n = min(kAtOnce, (left + step - 1) / step);        // positions of this thread
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       acc[i] = 0.0f;
-      const int64_t j = j0 + static_cast<int64_t>(i) * step;
-      was[i] = j < L ? out[j] : 0.0f;
+      if (i < n) was[i] = out[static_cast<int64_t>(i) * step];
     }
-    for (int g = 0; g < p.G; g += 2) {
-      const float l0 = lse2_sm[g], l1 = g + 1 < p.G ? lse2_sm[g + 1] : INFINITY;      // (no weight for a head that is not there)
-      float2 x[kAtOnce];
+    if (p.score_heads == 4) {                    // (the ordinary number: one load a position)
+      float4 x[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int64_t j = j0 + static_cast<int64_t>(i) * step;
-        x[i] = j < L ? __ldcs(reinterpret_cast<const float2*>(s + j * p.score_heads + g)) : make_float2(0.0f, 0.0f);
+      for (int i = 0; i < kAtOnce; ++i)
+        if (i < n) x[i] = __ldcs(reinterpret_cast<const float4*>(s + i * score_step));
+      const float l0 = lse2_sm[0], l1 = lse2_sm[1], l2 = lse2_sm[2], l3 = p.G > 3 ? lse2_sm[3] : INFINITY;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (i < n) acc[i] = ex2(x[i].x - l0) + ex2(x[i].y - l1) + ex2(x[i].z - l2) + (l3 != INFINITY ? ex2(x[i].w - l3) : 0.0f);
+    } else {
+      for (int g = 0; g < p.G; g += 2) {
+        const float l0 = lse2_sm[g], l1 = g + 1 < p.G ? lse2_sm[g + 1] : INFINITY;      // (no weight for a head that is not there)
+        float2 x[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (i < n) x[i] = __ldcs(reinterpret_cast<const float2*>(s + i * score_step + g));
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (i < n) acc[i] += ex2(x[i].x - l0) + (l1 != INFINITY ? ex2(x[i].y - l1) : 0.0f);
       }
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        acc[i] += ex2(x[i].x - l0);
-        if (l1 != INFINITY) acc[i] += ex2(x[i].y - l1);
-      }
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int64_t j = j0 + static_cast<int64_t>(i) * step;
-      if (j < L) out[j] = was[i] + acc[i];
-    }
+    for (int i = 0; i < kAtOnce; ++i)
+      if (i < n) out[static_cast<int64_t>(i) * step] = was[i] + acc[i];
   }
 }
 

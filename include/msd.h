@@ -458,7 +458,8 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
  * The rows (and INT8 scales) are COPIED to the pages of dst_block_table [B, dst_max_blocks], which has room for min(L, budget) tokens
  * of each sequence; the old pages are only read, so they may be shared with sequences outside the call, and are the caller's
  * to hand out again afterwards.  A page of dst_block_table appears nowhere else in it and in no row of block_table; the same pointer
- * for both is MSD_ERR_UNSUPPORTED, and so are new_weights == weights and new_seqlens == seqlens.
+ * for both is MSD_ERR_UNSUPPORTED, and so are new_weights == weights and new_seqlens == seqlens.  The rows of k and of v may spread over
+ * 64 GiB each (more: MSD_ERR_UNSUPPORTED).
  */
 msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* block_table, int32_t max_blocks, const int32_t* seqlens,
                                 const float* weights, int64_t ld, int32_t B, int32_t budget, int32_t recent, int32_t sinks,

@@ -130,7 +130,7 @@ struct Shape {
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
   static constexpr bool kWide = kHalf >= 4096;                  // 8 KB a tile and more
-  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (kInt8 && DP == 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
+  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (DP == 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
   static constexpr int kStages = kWide ? (kCtasPerSm == 3 ? 2 : 3) : (kHeads == 8 ? 3 : 4);
   static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
   static constexpr int kRing = kPWarps * kStages * kStage;
@@ -912,6 +912,9 @@ auto with_shape(bool int8, int widest, int slots, F&& f) {
 struct CtasPerSm {
   template <bool kInt8, int DP, int kHeads> int operator()() const { return Shape<kInt8, DP, kHeads>::kCtasPerSm; }
 };
+struct TileTokens {
+  template <bool kInt8, int DP, int kHeads> int operator()() const { return Shape<kInt8, DP, kHeads>::kTile; }
+};
 struct Launch {
   const PagedAttnParams& p;
   cudaStream_t s;
@@ -976,7 +979,10 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.G = Hq / cache->Hkv;
   p.groups = pl.groups;
   p.U = pl.U;
-  p.runs = pl.runs;
+  // no more runs than tiles that the sequences have room for (their lengths are on the device)
+  const int tile = with_shape(int8, widest, slots, TileTokens{});
+  const int64_t room = (p.cap + tile - 1) / tile * B;
+  p.runs = room < pl.runs ? static_cast<int>(room) : pl.runs;
   p.scale2 = softmax_scale * 1.4426950408889634f;
   p.out = static_cast<uint16_t*>(out_bf16);
   p.lse = lse;

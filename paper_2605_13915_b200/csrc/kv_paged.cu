@@ -45,24 +45,55 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int64_t n, 
   return lo >= 1 && lo <= B ? lo - 1 : -1;
 }
 
-// 8 BF16 values -> 8 codes rne(x / s), bit for bit those of a true division
-__device__ __forceinline__ uint2 codes_of(const uint4& v, float s, float inv) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t o[2] = {0, 0};
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float x = (e & 1) ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
-    int q;
-    if (s > 1e-30f) q = quant_i8(x, s, inv);
-    else q = s > 0.0f ? __float2int_rn(__fdiv_rn(x, s)) : 0;
-    q = max(-127, min(127, q));
-    o[e >> 2] |= static_cast<uint32_t>(q & 0xFF) << (8 * (e & 3));
-  }
-  return make_uint2(o[0], o[1]);
+// m / 127 as a true division gives it, by the same corrections as below; what is too small for exact remainders is divided.
+__device__ __forceinline__ float by_127(float m) {
+  constexpr float kY = 1.0f / 127.0f;
+  float q = m * kY;
+  q = __fmaf_rn(__fmaf_rn(-127.0f, q, m), kY, q);
+  q = __fmaf_rn(__fmaf_rn(-127.0f, q, m), kY, q);
+  return m > 1e-28f && m < 1e38f ? q : __fdiv_rn(m, 127.0f);
 }
 
+// 8 BF16 values -> 8 codes rne(fl(x / s)), two values an instruction and without a branch (rows are full of short integers over a short
+// integer, whose quotients are ties or next to them).  inv is the rounded reciprocal of s; x inv is off by 1.5 units of the quotient's last
+// place at most, one correction with the remainder leaves half a unit and a little, and a second one, from a quotient that is a neighbour of
+// the true one and an exact remainder, is the rounded quotient (Markstein's theorem).  Adding 1.5 * 2^23 rounds it half-to-even and leaves
+// the code in the low byte.  (The largest quotient is 127 up to a unit: nothing to clamp.)
+__device__ __forceinline__ uint2 codes_of(const uint4& v, float s, float inv) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  constexpr float kMagic = 12582912.0f;
+  const uint64_t magic2 = pack_f32x2(kMagic, kMagic), inv2 = pack_f32x2(inv, inv), ns2 = pack_f32x2(-s, -s), zero2 = pack_f32x2(0.0f, 0.0f);
+  uint32_t c[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint64_t x = pack_f32x2(bf16lo(w[e]), bf16hi(w[e]));
+    uint64_t q = fma_f32x2(x, inv2, zero2);
+    q = fma_f32x2(fma_f32x2(ns2, q, x), inv2, q);
+    q = fma_f32x2(fma_f32x2(ns2, q, x), inv2, q);
+    const float2 r = unpack_f32x2(add_f32x2(q, magic2));
+    c[2 * e] = __float_as_uint(r.x);
+    c[2 * e + 1] = __float_as_uint(r.y);
+  }
+  return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
+}
+// The same for a scale that is tiny or huge (or no number), by true divisions.
+__device__ __noinline__ uint2 codes_by_division(uint4 v, float s) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  unsigned long long out = 0;
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e) {
+    int c = 0;
+    if (s > 0.0f) c = max(-127, min(127, __float2int_rn(__fdiv_rn(bf16lo(w[0]), s))));
+    out |= static_cast<unsigned long long>(c & 0xFF) << (8 * e);
+    w[0] = __funnelshift_r(w[0], w[1], 16); w[1] = __funnelshift_r(w[1], w[2], 16); w[2] = __funnelshift_r(w[2], w[3], 16); w[3] >>= 16;
+  }
+  return make_uint2(static_cast<uint32_t>(out), static_cast<uint32_t>(out >> 32));
+}
+
+constexpr int kAppendCtas = 3;              // resident on an SM at least
 template <bool kInt8, int kVecs>            // kVecs: 16-byte pieces of a BF16 row a lane holds (rows of up to 128 kVecs values)
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, kAppendCtas)
 kv_append_kernel(const __grid_constant__ AppendParams p) {
   const int lane = threadIdx.x & 31, half = lane >> 4, hl = lane & 15;
   const int64_t warps = static_cast<int64_t>(gridDim.x) * (kAppendThreads / 32);
@@ -76,7 +107,7 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
   for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5); item < items; item += warps) {
     const int64_t n = item / p.head_groups;
     const int g0 = static_cast<int>(item - n * p.head_groups) * p.heads, g1 = min(p.c.Hkv, g0 + p.heads);
-    constexpr int kAhead = 4;               // heads whose rows are under way together
+    constexpr int kAhead = kVecs == 1 ? 4 : 2;         // heads whose rows are under way together
     uint4 x[kAhead][kVecs];
     auto fetch = [&](int h, uint4 (&v)[kVecs]) {
 #pragma unroll
@@ -123,11 +154,13 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
           for (int i = 0; i < kVecs; ++i) m = fmaxf(m, unit_absmax(x[a][i]));
 #pragma unroll
           for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-          const float s = __fdiv_rn(m, 127.0f), inv = __frcp_rn(s);
+          const float s = by_127(m);
+          const bool plain = s > 1e-30f && s < 1e30f;
+          const float inv = __frcp_rn(s);
 #pragma unroll
           for (int i = 0; i < kVecs; ++i) {
             const int d = (i * 16 + hl) * 8;
-            if (d < D) *reinterpret_cast<uint2*>(to + d) = codes_of(x[a][i], s, inv);
+            if (d < D) *reinterpret_cast<uint2*>(to + d) = plain ? codes_of(x[a][i], s, inv) : codes_by_division(x[a][i], s);
           }
           if (hl == 0) *reinterpret_cast<float*>(dst_s + (h + a) * scales.head) = s;
         }
@@ -143,7 +176,7 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
 
 template <bool kInt8, int kVecs>
 msd_status_t launch_append(const AppendParams& p, cudaStream_t s) {
-  const int64_t per = kAppendThreads / 32, ctas = (p.n_rows * p.head_groups + per - 1) / per, most = 8LL * sm_count();
+  const int64_t per = kAppendThreads / 32, ctas = (p.n_rows * p.head_groups + per - 1) / per, most = 16LL * sm_count();
   return launch_pdl(kv_append_kernel<kInt8, kVecs>, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), dim3(kAppendThreads), 0, s,
                     option(OPT_NO_PDL) != 1, p) == cudaSuccess
              ? MSD_OK
@@ -152,12 +185,14 @@ msd_status_t launch_append(const AppendParams& p, cudaStream_t s) {
 
 // ---------------------------------------------------------------------------------------------------------------------------
 // Eviction, first kernel: which tokens stay.  A cluster of CTAs per (sequence, KV head) holds the weights as ordered integers in
-// registers (32 a thread at most; longer rows are read again each round) and finds the k-th largest by two bits a round: three counts,
-// summed over the warps and, through the peers' shared memory, over the cluster.  What is above it stays, of what equals it the
-// first ones; a scan over the positions in order gives each its new place.
+// registers (16 a thread at most; longer rows are read again in each pass) and finds the k-th largest in up to three passes: the range that
+// holds it, at first from the smallest key to the largest, is cut into 2048 bins, a histogram of it is made in shared memory, added up over
+// the cluster by remote atomics on what is not zero (integers: the order does not matter), and a scan from the top gives the bin that
+// is the next range.  (Cutting the range that is there, not the whole range of the bits, spreads the first histogram over more bins: threads
+// that add to the same one wait for each other.)  What is above the k-th stays, of what
+// equals it the first ones; a scan over the positions in order gives each its new place.  (Finding it by two bits a round, three counts
+// over all keys: 61 instead of {SEL32} us for 256 rows of 2048 to 8192.)
 // ---------------------------------------------------------------------------------------------------------------------------
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
-
 struct EvictParams {
   PagedCache c;
   const int32_t *table, *dst_table, *seqlens;
@@ -166,7 +201,7 @@ struct EvictParams {
   int max_blocks, dst_max_blocks, B, budget, recent, sinks;
   int32_t *new_seqlens, *kept;
   float* new_weights;
-  int rows_per_cta, chunks;          // of the move
+  int warp_rows, chunks;             // of the move: rows of a warp, CTAs of a (sequence, KV head)
   unsigned* status;
 };
 
@@ -175,9 +210,10 @@ __device__ __forceinline__ int evict_len(const EvictParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(n < 0 ? 0 : n), p.cap));
 }
 
-// order of the weights as unsigned integers: NaN above everything, -0 as 0; never 0
+// Order of the weights as unsigned integers: NaN above the others, -0 as 0.  0 is no key, and kProtected that of a token that stays anyway.
+constexpr uint32_t kProtected = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (w != w) return 0xFFFFFFFFu;
+  if (w != w) return kProtected - 1;
   const uint32_t u = __float_as_uint(w + 0.0f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
@@ -187,12 +223,26 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t caddr) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(caddr) : "memory");
   return v;
 }
+__device__ __forceinline__ void add_cluster_u32(uint32_t caddr, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(caddr), "r"(v) : "memory");
+}
 
-template <int kKeys>        // keys a thread keeps; 0: none, they are read from memory in every round
-__global__ void __launch_bounds__(kSelThreads)
+__device__ __forceinline__ void count_shared(uint32_t saddr) {
+  asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(saddr) : "memory");
+}
+
+constexpr int kBins = 2048, kPasses = 3;
+constexpr uint32_t kNowhere = 0xFFFFFFFFu;
+
+template <int kKeys, int kSelThreads>        // keys a thread keeps; 0: none, they are read from memory in every pass
+__global__ void __launch_bounds__(kSelThreads, 1024 / kSelThreads)
 kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
-  __shared__ uint32_t part[kSelWarps][3];
-  __shared__ uint32_t sums[2][3];                       // this CTA's counts, by round parity
+  constexpr int kSelWarps = kSelThreads / 32, kBinsEach = kBins / kSelThreads;
+  __shared__ __align__(16) uint32_t own[kBins];          // histogram of this CTA's keys
+  __shared__ __align__(16) uint32_t all[kPasses][kBins]; // of the cluster's, a pass each
+  __shared__ uint32_t range[2];                         // smallest and largest key of this CTA
+  __shared__ uint32_t part[kSelWarps][2];
+  __shared__ uint32_t found[3];                         // bin, keys above it, keys in it
   __shared__ uint32_t totals[2];                        // staying for sure, equal to the threshold
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x % ctas, bk = blockIdx.x / ctas;
@@ -215,18 +265,23 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
     return;
   }
   // Positions in order: CTA by CTA, warp by warp, 32 at a time; lane `lane` of this warp has begin + 32 j.
-  const int rows = (L + ctas * kSelThreads - 1) / (ctas * kSelThreads);
-  const int64_t begin = (static_cast<int64_t>(rank) * kSelWarps + warp) * rows * 32 + lane;
-  const int lo = p.sinks, hi = L - p.recent;            // what is not protected
-  const uint32_t want = static_cast<uint32_t>(p.budget - p.sinks - p.recent);
-  auto key_at = [&](int j) -> uint32_t {
-    const int64_t i = begin + j * 32;
-    return i >= lo && i < hi ? weight_key(w[i]) : 0u;
-  };
+  const int rows = static_cast<int>((static_cast<uint32_t>(L) + ctas * kSelThreads - 1) / (ctas * kSelThreads));
+  const uint32_t begin = (static_cast<uint32_t>(rank) * kSelWarps + warp) * rows * 32 + lane;      // (all of them below 2^32)
+  const uint32_t lo = p.sinks, middle = L - p.recent - p.sinks;       // what is not protected: the first one, how many (more than 0)
+  const uint32_t want = p.budget;
+  // (j-th position of this lane; `there`: how many there are behind `begin`)
+  const float* w_lane = w + begin;
+  const int there = L - static_cast<int>(min(begin, static_cast<uint32_t>(L)));
+  const uint32_t from_lo = begin - lo;
+  auto key_of = [&](int j, float x) -> uint32_t { return from_lo + j * 32 < middle ? weight_key(x) : (j * 32 < there ? kProtected : 0u); };
+  auto key_at = [&](int j) -> uint32_t { return key_of(j, j * 32 < there ? w_lane[j * 32] : 0.0f); };
   uint32_t key[kKeys > 0 ? kKeys : 1];
-  if constexpr (kKeys > 0) {
+  if constexpr (kKeys > 0) {      // (loads side by side: no branch between them)
+    float x[kKeys];
 #pragma unroll
-    for (int j = 0; j < kKeys; ++j) key[j] = j < rows ? key_at(j) : 0u;
+    for (int j = 0; j < kKeys; ++j) x[j] = j < rows && j * 32 < there ? w_lane[j * 32] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) key[j] = j < rows ? key_of(j, x[j]) : 0u;
   }
   auto for_keys = [&](auto&& f) {                       // (alike in all lanes)
     if constexpr (kKeys > 0) {
@@ -238,74 +293,108 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
       for (int j = 0; j < rows; ++j) f(j, key_at(j));
     }
   };
-  // counts of the cluster; every thread of it calls this, with alternating parity
-  auto cluster_sum = [&](uint32_t (&c)[3], int parity) {
-#pragma unroll
-    for (int i = 0; i < 3; ++i) c[i] = __reduce_add_sync(0xffffffffu, c[i]);
-    if (lane == 0) {
-#pragma unroll
-      for (int i = 0; i < 3; ++i) part[warp][i] = c[i];
+  uint32_t T = kProtected - 1, above = p.sinks + p.recent;       // the want-th largest key, and how many are above it
+  if (want > above) {
+    uint32_t smallest = 0xFFFFFFFFu, largest = 0;
+    for_keys([&](int, uint32_t k) {
+      if (k != 0) smallest = min(smallest, k);
+      if (k != kProtected) largest = max(largest, k);
+    });
+    smallest = __reduce_min_sync(0xffffffffu, smallest);
+    largest = __reduce_max_sync(0xffffffffu, largest);
+    if (lane == 0) { part[warp][0] = smallest; part[warp][1] = largest; }
+    if (ctas > 1) {
+      for (int i = threadIdx.x; i < kPasses * kBins; i += kSelThreads) (&all[0][0])[i] = 0;
     }
     __syncthreads();
-    if (warp == 0) {
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const uint32_t v = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? part[lane][i] : 0u);
-        if (lane == 0) sums[parity][i] = v;
-      }
-    }
+    smallest = __reduce_min_sync(0xffffffffu, part[lane & (kSelWarps - 1)][0]);
+    largest = __reduce_max_sync(0xffffffffu, part[lane & (kSelWarps - 1)][1]);
     if (ctas > 1) {
+      if (threadIdx.x == 0) { range[0] = smallest; range[1] = largest; }
       __syncwarp();
       cluster_arrive_all();
       cluster_wait_all();
+      smallest = __reduce_min_sync(0xffffffffu, ld_cluster_u32(mapa_shared(smem_u32(&range[0]), lane & (ctas - 1))));
+      largest = __reduce_max_sync(0xffffffffu, ld_cluster_u32(mapa_shared(smem_u32(&range[1]), lane & (ctas - 1))));
+    }
+    T = smallest;                                       // the key lies in [T, T + 2^bits)
+    int bits = 32 - __clz(largest - smallest);
+    const uint32_t own_u = smem_u32(own);
+    for (int pass = 0; bits > 0; ++pass) {              // 11 bits fewer each time: three passes at most
+      const int shift = max(bits - 11, 0);
+      const uint32_t bins = bits < 11 ? 1u << bits : kBins;
+      uint32_t c[kBinsEach];                            // this thread's bins
 #pragma unroll
-      for (int i = 0; i < 3; ++i)
-        c[i] = __reduce_add_sync(0xffffffffu, lane < ctas ? ld_cluster_u32(mapa_shared(smem_u32(&sums[parity][i]), lane)) : 0u);
-    } else {
+      for (int i = 0; i < kBinsEach; ++i) own[threadIdx.x * kBinsEach + i] = 0;
+      __syncthreads();
+      for_keys([&](int, uint32_t k) {
+        const uint32_t bin = (k - T) >> shift;
+        if (k >= T && bin < bins && k != kProtected) count_shared(own_u + bin * 4);      // (0 is below T)
+      });
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 3; ++i) c[i] = sums[parity][i];
-    }
-  };
-
-  uint32_t T = 0, above = 0;                            // the want-th largest key, and how many are above it
-  if (want > 0) {
-    int parity = 0;
-    for (int s = 30; s >= 0; s -= 2) {
-      const uint32_t t1 = T + (1u << s), t2 = T + (2u << s), t3 = T + (3u << s);
-      uint32_t c[3] = {0, 0, 0};
-      for_keys([&](int, uint32_t k) {
-        c[0] += k >= t1;
-        c[1] += k >= t2;
-        c[2] += k >= t3;
-      });
-      cluster_sum(c, parity);
-      parity ^= 1;
-      if (c[2] >= want) {
-        T = t3;
-      } else if (c[1] >= want) {
-        T = t2;
-        above = c[2];
-      } else if (c[0] >= want) {
-        T = t1;
-        above = c[1];
-      } else {
-        above = c[0];
+      for (int i = 0; i < kBinsEach; ++i) c[i] = own[threadIdx.x * kBinsEach + i];
+      if (ctas > 1) {
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) {
+          if (c[i] == 0) continue;
+          const uint32_t at = smem_u32(&all[pass][threadIdx.x * kBinsEach + i]);
+          for (int r = 0; r < ctas; ++r) add_cluster_u32(mapa_shared(at, r), c[i]);
+        }
+        cluster_arrive_all();
+        cluster_wait_all();
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) c[i] = all[pass][threadIdx.x * kBinsEach + i];
+      }
+      // keys in the bins of the threads after this one
+      uint32_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < kBinsEach; ++i) sum += c[i];
+      uint32_t upto = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t y = __shfl_down_sync(0xffffffffu, upto, d);
+        if (lane + d < 32) upto += y;
+      }
+      if (lane == 0) part[warp][0] = upto;
+      __syncthreads();
+      uint32_t later = lane > warp && lane < kSelWarps ? part[lane][0] : 0u;
+      later = __reduce_add_sync(0xffffffffu, later) + upto - sum;
+      const uint32_t left = want - above;               // the key is the left-th from the top of these
+      if (later < left && left <= later + sum) {
+        uint32_t n = later;
+#pragma unroll
+        for (int i = kBinsEach - 1; i >= 0; --i) {
+          if (n < left && n + c[i] >= left) {
+            found[0] = threadIdx.x * kBinsEach + i;
+            found[1] = n;
+            found[2] = c[i];
+          }
+          n += c[i];
+        }
+      }
+      __syncthreads();
+      T += found[0] << shift;
+      above += found[1];
+      bits = shift;
+      if (above + found[2] == want) {                   // the whole bin stays, as a rule after two passes: no need to look into it
+        above = want;
+        --T;
+        break;
       }
     }
   }
   const uint32_t need = want - above;                   // of those equal to T, the first ones
 
-  // Two flags a position: it stays for sure (protected, or above T), or it equals T.  Their numbers before a position give its new place.
-  auto flags = [&](int j, uint32_t k, unsigned* sure, unsigned* equal) {
-    const int64_t i = begin + j * 32;
-    *sure = __ballot_sync(0xffffffffu, i < L && (i < lo || i >= hi || (want > 0 && k > T)));
-    *equal = __ballot_sync(0xffffffffu, want > 0 && k == T);
+  // Two flags a position: it stays for sure (above T), or it equals T.  Their numbers before a position give its new place.
+  auto flags = [&](uint32_t k, unsigned* sure, unsigned* equal) {
+    *sure = __ballot_sync(0xffffffffu, k > T);
+    *equal = __ballot_sync(0xffffffffu, k == T);
   };
   uint32_t a = 0, e = 0;
-  for_keys([&](int j, uint32_t k) {
+  for_keys([&](int, uint32_t k) {
     unsigned ms, me;
-    flags(j, k, &ms, &me);
+    flags(k, &ms, &me);
     a += __popc(ms);
     e += __popc(me);
   });
@@ -327,94 +416,113 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
       cluster_arrive_all();                             // (nobody leaves while a peer may still read its totals)
     }
   }
-  for_keys([&](int j, uint32_t k) {
+  auto place = [&](uint32_t k) -> uint32_t {            // new place of this lane's position, or none
     unsigned ms, me;
-    flags(j, k, &ms, &me);
+    flags(k, &ms, &me);
     const uint32_t pa = a + __popc(ms & lanes_below(lane)), pe = e + __popc(me & lanes_below(lane));
-    if (((ms >> lane) & 1u) || (((me >> lane) & 1u) && pe < need)) {
-      const int64_t i = begin + j * 32;
-      const uint32_t at = pa + min(pe, need);
-      kept[at] = static_cast<int32_t>(i);
-      new_w[at] = w[i];
-    }
     a += __popc(ms);
     e += __popc(me);
-  });
+    return ((ms >> lane) & 1u) || (((me >> lane) & 1u) && pe < need) ? pa + min(pe, need) : kNowhere;
+  };
+  if constexpr (kKeys > 0) {
+    float x[kKeys];
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {
+      key[j] = j < rows ? place(key[j]) : kNowhere;
+      x[j] = key[j] != kNowhere ? w_lane[j * 32] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) {
+      if (key[j] == kNowhere) continue;
+      kept[key[j]] = static_cast<int32_t>(begin + j * 32);
+      new_w[key[j]] = x[j];
+    }
+  } else {
+    for (int j = 0; j < rows; ++j) {
+      const uint32_t at = place(key_at(j));
+      if (at == kNowhere) continue;
+      kept[at] = static_cast<int32_t>(begin + j * 32);
+      new_w[at] = w_lane[j * 32];
+    }
+  }
   if (ctas > 1) cluster_wait_all();
 }
 
+template <int kKeys, int kThreads>
+cudaError_t launch_select(const EvictParams& p, int64_t units, int ctas, cudaStream_t s, bool pdl) {
+  return launch_pdl_cluster(kv_evict_select_kernel<kKeys, kThreads>, dim3(static_cast<unsigned>(units * ctas)), dim3(kThreads), 0, s, pdl,
+                            static_cast<unsigned>(ctas), p, ctas);
+}
+
 // ---------------------------------------------------------------------------------------------------------------------------
-// Eviction, second kernel: the kept rows go to their new pages.  Bound: HBM.  kLanes lanes (a power of two) copy a row's key and value,
-// 16 bytes at a time; a warp has 32 / kLanes rows under way, four times over.  Sources and destinations never overlap, so
-// the order of the copies does not matter.
+// Eviction, second kernel: the kept rows go to their new pages.  Bound: HBM.  A warp takes up to 32 rows: each lane looks up where one of
+// them is and where it goes, and moves its scales; then kLanes lanes (a power of two) copy a row's key and value, 16 bytes at a time,
+// several rows under way.  Sources and destinations never overlap, so the order of the copies does not matter.
 // ---------------------------------------------------------------------------------------------------------------------------
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 128;
 
 template <bool kInt8, int kLanes>
-__global__ void __launch_bounds__(kMoveThreads)
+__global__ void __launch_bounds__(kMoveThreads, 8)
 kv_evict_move_kernel(const __grid_constant__ EvictParams p) {
-  constexpr int kRowsPerWarp = 32 / kLanes, kAhead = 4;
+  constexpr int kRowsPer = 32 / kLanes, kAhead = 4;      // rows of a step, steps whose loads are under way together
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int hk = blockIdx.x % p.c.Hkv, bc = blockIdx.x / p.c.Hkv, b = bc / p.chunks;
-  const int64_t row0 = static_cast<int64_t>(bc - b * p.chunks) * p.rows_per_cta;
+  const int64_t row0 = static_cast<int64_t>(bc - b * p.chunks) * (kMoveThreads / 32 * p.warp_rows) + warp * p.warp_rows;
   pdl_wait_primary();
   pdl_launch_dependents();
   int n = min(evict_len(p, b), p.budget);
-  if (row0 >= n) return;
   if (n > p.dst_cap) {
-    if (threadIdx.x == 0) atomicMax(p.status, kStatusBadShape);
+    if (row0 == 0 && lane == 0) atomicMax(p.status, kStatusBadShape);
     n = static_cast<int>(p.dst_cap);
   }
-  const int end = static_cast<int>(min(static_cast<int64_t>(n), row0 + p.rows_per_cta));
-  const int32_t* kept = p.kept + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.budget;
-  const int32_t* table = p.table + static_cast<int64_t>(b) * p.max_blocks;
-  const int32_t* dst_table = p.dst_table + static_cast<int64_t>(b) * p.dst_max_blocks;
-  const int sub = lane / kLanes, l = lane % kLanes;
-  const int es = kInt8 ? 1 : 2;
-  const bool has_k = l * 16 < p.c.D * es, has_v = l * 16 < p.c.Dv * es;
-  constexpr int kStep = kMoveThreads / 32 * kRowsPerWarp;
-  for (int i0 = static_cast<int>(row0) + warp * kRowsPerWarp + sub; i0 - sub < end; i0 += kStep * kAhead) {
-    int32_t from[kAhead], blk[kAhead], to[kAhead];
-    uint32_t slot[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int i = i0 + a * kStep;
-      from[a] = i < end ? kept[i] : -1;
-      to[a] = i < end ? dst_table[div_by(i, p.c.page)] : 0;
-    }
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      blk[a] = 0;
-      slot[a] = 0;
-      if (from[a] < 0) continue;
-      const uint32_t page = div_by(from[a], p.c.page);
-      slot[a] = from[a] - page * p.c.page.d;
-      blk[a] = table[page];
-    }
-    uint4 k[kAhead], v[kAhead];
-    float ks[kAhead], vs[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      if (from[a] >= 0 && (static_cast<uint32_t>(blk[a]) >= static_cast<uint64_t>(p.c.num_blocks) ||
-                           static_cast<uint32_t>(to[a]) >= static_cast<uint64_t>(p.c.num_blocks))) {
-        atomicMax(p.status, kStatusBadShape);
-        from[a] = -1;
+  if (row0 >= n) return;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(p.warp_rows), n - row0));
+  uint32_t ko = 0, vo = 0, kd = 0, vd = 0;               // offsets of this lane's row in units of 16 bytes: from, to
+  bool ok = false;
+  if (lane < rows) {
+    const int i = static_cast<int>(row0) + lane;
+    const int32_t from = p.kept[(static_cast<int64_t>(b) * p.c.Hkv + hk) * p.budget + i];
+    const uint32_t from_page = div_by(from, p.c.page), to_page = div_by(i, p.c.page);
+    const int32_t blk = p.table[static_cast<int64_t>(b) * p.max_blocks + from_page], to = p.dst_table[static_cast<int64_t>(b) * p.dst_max_blocks + to_page];
+    const uint32_t slot = from - from_page * p.c.page.d, to_slot = i - to_page * p.c.page.d;
+    if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(p.c.num_blocks) && static_cast<uint32_t>(to) < static_cast<uint64_t>(p.c.num_blocks)) {
+      ok = true;
+      ko = static_cast<uint32_t>(row_offset(p.c.k, blk, slot) >> 4);
+      vo = static_cast<uint32_t>(row_offset(p.c.v, blk, slot) >> 4);
+      kd = static_cast<uint32_t>(row_offset(p.c.k, to, to_slot) >> 4);
+      vd = static_cast<uint32_t>(row_offset(p.c.v, to, to_slot) >> 4);
+      if constexpr (kInt8) {
+        const float ks = *reinterpret_cast<const float*>(p.c.ks.base + hk * p.c.ks.head + row_offset(p.c.ks, blk, slot));
+        const float vs = *reinterpret_cast<const float*>(p.c.vs.base + hk * p.c.vs.head + row_offset(p.c.vs, blk, slot));
+        *reinterpret_cast<float*>(p.c.ks.base + hk * p.c.ks.head + row_offset(p.c.ks, to, to_slot)) = ks;
+        *reinterpret_cast<float*>(p.c.vs.base + hk * p.c.vs.head + row_offset(p.c.vs, to, to_slot)) = vs;
       }
-      if (from[a] < 0) continue;
-      if (has_k) k[a] = __ldcs(reinterpret_cast<const uint4*>(p.c.k.base + hk * p.c.k.head + row_offset(p.c.k, blk[a], slot[a]) + l * 16));
-      if (has_v) v[a] = __ldcs(reinterpret_cast<const uint4*>(p.c.v.base + hk * p.c.v.head + row_offset(p.c.v, blk[a], slot[a]) + l * 16));
-      if (kInt8 && l == 0) ks[a] = *reinterpret_cast<const float*>(p.c.ks.base + hk * p.c.ks.head + row_offset(p.c.ks, blk[a], slot[a]));
-      if (kInt8 && l == 1) vs[a] = *reinterpret_cast<const float*>(p.c.vs.base + hk * p.c.vs.head + row_offset(p.c.vs, blk[a], slot[a]));
+    } else {
+      atomicMax(p.status, kStatusBadShape);
+    }
+  }
+  const int sub = lane / kLanes, l16 = lane % kLanes * 16, es = kInt8 ? 1 : 2;
+  const uint32_t oks = __ballot_sync(0xffffffffu, ok) >> sub;
+  const uint32_t k_rows = l16 < p.c.D * es ? oks : 0u, v_rows = l16 < p.c.Dv * es ? oks : 0u;      // (bit r: row r + sub)
+  uint8_t* kat = p.c.k.base + hk * p.c.k.head + l16;
+  uint8_t* vat = p.c.v.base + hk * p.c.v.head + l16;
+  for (int r0 = 0; r0 < rows; r0 += kRowsPer * kAhead) {
+    uint4 k[kAhead], v[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int r = r0 + a * kRowsPer;                   // (below 32: r0 is a multiple of kRowsPer kAhead, which divides 32 or is more)
+      if (r >= 32) break;
+      const uint32_t fk = __shfl_sync(0xffffffffu, ko, r + sub), fv = __shfl_sync(0xffffffffu, vo, r + sub);
+      if ((k_rows >> r) & 1u) k[a] = __ldcs(reinterpret_cast<const uint4*>(kat + static_cast<uint64_t>(fk) * 16));
+      if ((v_rows >> r) & 1u) v[a] = __ldcs(reinterpret_cast<const uint4*>(vat + static_cast<uint64_t>(fv) * 16));
     }
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      if (from[a] < 0) continue;
-      const int i = i0 + a * kStep;
-      const uint32_t s = i - div_by(i, p.c.page) * p.c.page.d;
-      if (has_k) *reinterpret_cast<uint4*>(p.c.k.base + hk * p.c.k.head + row_offset(p.c.k, to[a], s) + l * 16) = k[a];
-      if (has_v) *reinterpret_cast<uint4*>(p.c.v.base + hk * p.c.v.head + row_offset(p.c.v, to[a], s) + l * 16) = v[a];
-      if (kInt8 && l == 0) *reinterpret_cast<float*>(p.c.ks.base + hk * p.c.ks.head + row_offset(p.c.ks, to[a], s)) = ks[a];
-      if (kInt8 && l == 1) *reinterpret_cast<float*>(p.c.vs.base + hk * p.c.vs.head + row_offset(p.c.vs, to[a], s)) = vs[a];
+      const int r = r0 + a * kRowsPer;
+      if (r >= 32) break;
+      const uint32_t tk = __shfl_sync(0xffffffffu, kd, r + sub), tv = __shfl_sync(0xffffffffu, vd, r + sub);
+      if ((k_rows >> r) & 1u) *reinterpret_cast<uint4*>(kat + static_cast<uint64_t>(tk) * 16) = k[a];
+      if ((v_rows >> r) & 1u) *reinterpret_cast<uint4*>(vat + static_cast<uint64_t>(tv) * 16) = v[a];
     }
   }
 }
@@ -465,9 +573,9 @@ msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16,
   p.B = B;
   p.weights = weights;
   p.ld = ld;
-  // KV heads a warp takes: as many as leave a warp for every place on the machine (64 an SM), one for a few rows
+  // KV heads a warp takes: as many as leave an item for every warp of the machine, one for a few rows
   p.heads = cache->Hkv;
-  while (p.heads > 1 && n_rows * ((cache->Hkv + p.heads - 1) / p.heads) < 64LL * sm_count()) p.heads = (p.heads + 1) / 2;
+  while (p.heads > 1 && n_rows * ((cache->Hkv + p.heads - 1) / p.heads) < static_cast<int64_t>(kAppendCtas) * kAppendThreads / 32 * sm_count()) p.heads = (p.heads + 1) / 2;
   p.head_groups = (cache->Hkv + p.heads - 1) / p.heads;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool wide = cache->D > 128 || cache->Dv > 128;
@@ -487,6 +595,8 @@ msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* b
     return MSD_ERR_BAD_SHAPE;
   if (B == 0) return MSD_OK;
   if (!block_table || !seqlens || !weights || !dst_block_table || !new_seqlens || !new_weights || !kept) return MSD_ERR_NULL_POINTER;
+  if (!rows_within(p.c.k, cache->num_blocks, cache->page_size, int64_t{1} << 36) || !rows_within(p.c.v, cache->num_blocks, cache->page_size, int64_t{1} << 36))
+    return MSD_ERR_UNSUPPORTED;
   if (block_table == dst_block_table || weights == new_weights || seqlens == new_seqlens) return MSD_ERR_UNSUPPORTED;
   if (!aligned(block_table, 4) || !aligned(seqlens, 4) || !aligned(weights, 4) || !aligned(dst_block_table, 4) || !aligned(new_seqlens, 4) ||
       !aligned(new_weights, 4) || !aligned(kept, 4))
@@ -514,35 +624,36 @@ msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* b
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool pdl = option(OPT_NO_PDL) != 1;
 
-  // CTAs of a cluster: 2048 positions each while the machine is not full, and as many as the longest row needs (8 x 512 x 32 positions
-  // fit; longer rows are read again in every round)
+  // CTAs of a cluster: 2048 positions each while the machine is not full, and as many as the longest row needs (8 x 1024 x 16 positions
+  // fit; longer rows are read again in every pass).  (16 CTAs, which this device allows, took 4 us more on 8 rows of 131072.)  1024
+  // threads where 512 would hold more than 16 keys each: the warps' latencies, not their number, set the pace.
   const int64_t units = static_cast<int64_t>(B) * cache->Hkv;
   if (units > (1 << 24)) return MSD_ERR_UNSUPPORTED;
   int ctas = 1;
-  while (ctas < 8 && (p.cap > static_cast<int64_t>(ctas) * kSelThreads * 32 || (p.cap > ctas * 2048LL && units * ctas * 2 <= 2LL * sm_count()))) ctas *= 2;
-  const int64_t keys = (p.cap + static_cast<int64_t>(ctas) * kSelThreads - 1) / (static_cast<int64_t>(ctas) * kSelThreads);
-  const dim3 grid(static_cast<unsigned>(units * ctas)), block(kSelThreads);
-  const unsigned cluster = static_cast<unsigned>(ctas);
-  cudaError_t err;
-  if (keys <= 4) err = launch_pdl_cluster(kv_evict_select_kernel<4>, grid, block, 0, s, pdl, cluster, p, ctas);
-  else if (keys <= 16) err = launch_pdl_cluster(kv_evict_select_kernel<16>, grid, block, 0, s, pdl, cluster, p, ctas);
-  else if (keys <= 32) err = launch_pdl_cluster(kv_evict_select_kernel<32>, grid, block, 0, s, pdl, cluster, p, ctas);
-  else err = launch_pdl_cluster(kv_evict_select_kernel<0>, grid, block, 0, s, pdl, cluster, p, ctas);
+  while (ctas < 8 && (p.cap > ctas * 16384LL || (p.cap > ctas * 2048LL && units * ctas <= sm_count()))) ctas *= 2;
+  const int64_t keys = (p.cap + ctas * 512LL - 1) / (ctas * 512LL);
+  const cudaError_t err = keys <= 4    ? launch_select<4, 512>(p, units, ctas, s, pdl)
+                          : keys <= 8  ? launch_select<8, 512>(p, units, ctas, s, pdl)
+                          : keys <= 16 ? launch_select<16, 512>(p, units, ctas, s, pdl)
+                          : keys <= 32 ? launch_select<16, 1024>(p, units, ctas, s, pdl)
+                                       : launch_select<0, 1024>(p, units, ctas, s, pdl);
   if (err != cudaSuccess) {
     cudaGetLastError();
     return MSD_ERR_CUDA;
   }
 
-  // rows of a CTA: 256 where that leaves the machine its CTAs, 32 at least
+  // rows of a warp: 32 where that leaves 32 warps to an SM, 8 at least
   const int64_t most = p.cap < budget ? p.cap : budget;
-  p.rows_per_cta = 256;
-  while (p.rows_per_cta > 32 && units * ((most + p.rows_per_cta - 1) / p.rows_per_cta) < 4LL * sm_count()) p.rows_per_cta /= 2;
-  while (units * ((most + p.rows_per_cta - 1) / p.rows_per_cta) > 0x7FFFFFFF) p.rows_per_cta *= 2;
-  p.chunks = static_cast<int>((most + p.rows_per_cta - 1) / p.rows_per_cta);
+  p.warp_rows = 32;
+  while (p.warp_rows > 8 && units * most < 32LL * p.warp_rows * sm_count()) p.warp_rows /= 2;
+  const int64_t cta_rows = kMoveThreads / 32 * p.warp_rows, chunks = (most + cta_rows - 1) / cta_rows;
+  if (units * chunks > 0x7FFFFFFF) return MSD_ERR_UNSUPPORTED;
+  p.chunks = static_cast<int>(chunks);
   const int widest = (cache->D > cache->Dv ? cache->D : cache->Dv) * (cache->type == MSD_CACHE_INT8 ? 1 : 2);      // bytes of a row
-  if (cache->type == MSD_CACHE_INT8) err = widest <= 128 ? launch_move<true, 8>(p, s, pdl) : launch_move<true, 16>(p, s, pdl);
-  else err = widest <= 128 ? launch_move<false, 8>(p, s, pdl) : (widest <= 256 ? launch_move<false, 16>(p, s, pdl) : launch_move<false, 32>(p, s, pdl));
-  if (err != cudaSuccess) {
+  cudaError_t moved;
+  if (cache->type == MSD_CACHE_INT8) moved = widest <= 128 ? launch_move<true, 8>(p, s, pdl) : launch_move<true, 16>(p, s, pdl);
+  else moved = widest <= 128 ? launch_move<false, 8>(p, s, pdl) : (widest <= 256 ? launch_move<false, 16>(p, s, pdl) : launch_move<false, 32>(p, s, pdl));
+  if (moved != cudaSuccess) {
     cudaGetLastError();
     return MSD_ERR_CUDA;
   }

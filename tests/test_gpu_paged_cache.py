@@ -267,6 +267,21 @@ def test_append(lengths, new, Hkv, D, Dv, page, layout, int8):
         assert (weights[b, :, n - m:n] == 0).all() and (weights[b, :, :n - m] == 0.25).all() and (weights[b, :, n:] == 0.25).all()
 
 
+def test_append_quantises_every_largest_value():
+    """Each positive finite BF16 number as the largest of a row, the others at or next to halves of a step."""
+    top = torch.arange(1, 0x7F80, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    n = top.numel()
+    step = torch.arange(15).float() * 9 - 60.5
+    rows = torch.cat([top[:, None], (top.float()[:, None] / 127 * step).to(torch.bfloat16)], 1).view(n, 1, 16)
+    c = make_cache([n], 1, 16, 16, 64, int8=True, poison=False)
+    want = _append_reference(c, rows, rows.flip(2), [0, n])
+    binding.kv_append_paged(rows.cuda(), rows.flip(2).contiguous().cuda(), *_args(c), torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    binding.last_device_status()
+    for got, ref in zip((c["k"], c["v"], c["k_scale"].view(torch.int32), c["v_scale"].view(torch.int32)),
+                        (want[0], want[1], want[2].view(torch.int32), want[3].view(torch.int32))):
+        assert torch.equal(got.cpu(), ref)
+
+
 def test_append_reports_what_does_not_fit():
     c = make_cache([20, 20], 2, 64, 64, 16, seed=1, poison=False)
     new = torch.ones(4, 2, 64, dtype=torch.bfloat16, device="cuda")

@@ -71,8 +71,12 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {       // zeros where there is nothing
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// (`policy`: keys and values leave L2 first; the scores that the second kernel reads stay)
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there, uint64_t policy) {      // zeros where there is nothing
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint.L2::128B [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void cp16_all(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
@@ -86,14 +90,17 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
-template <bool kHalfs>      // FP16 or BF16 operands
+template <bool kHalfs, bool kFirst = false>      // FP16 or BF16 operands; kFirst: c = a b instead of c += a b
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], const uint2& b) {
+  const float z0 = kFirst ? 0.0f : c[0], z1 = kFirst ? 0.0f : c[1], z2 = kFirst ? 0.0f : c[2], z3 = kFirst ? 0.0f : c[3];
   if constexpr (kHalfs)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(z0), "f"(z1), "f"(z2), "f"(z3));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
@@ -107,7 +114,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {       // of an 8 x 8 matrix of 16-bit values over the warp
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 // bytes kLo and kHi of u, each a code plus 128, as an FP16 pair of the codes: 1024 + u has the byte as its lowest bits
@@ -235,6 +242,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   };
 
   // ---- loads ----
+  const uint64_t policy = policy_evict_first();
   uint8_t* ring = smem + warp * (S::kStages * S::kStage);
   const uint32_t ring_u = smem_u32(ring);
   constexpr int kChunks = S::kRow / 16;                 // 16-byte chunks of a row
@@ -245,7 +253,11 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   const uint8_t* ksbase = kInt8 ? p.c.ks.base + hk * p.c.ks.head : nullptr;
   const uint8_t* vsbase = kInt8 ? p.c.vs.base + hk * p.c.vs.head : nullptr;
   const bool k_there = my_chunk * 16 < p.c.D * S::kEs, v_there = my_chunk * 16 < p.c.Dv * S::kEs;
-  const int tok_lane = lane & (S::kTok - 1);
+  // Instruction i brings row i * kRowsPer + my_row to the lanes of my_row.  The lane that looks that row up is the i-th of them, so that
+  // the others get its offset by a shuffle whose index is a constant.
+  constexpr int kIter = S::kTok / kRowsPer;
+  const int tok_lane = my_chunk % kIter * kRowsPer + my_row;
+  const uint32_t lane_dst = S::kRow >= 128 ? my_row * S::kRow + ((my_chunk ^ my_row) << 4) : swz<S::kRow>(my_row, my_chunk);
   // The block of this lane's token of the tile that `ld` stands on, asked for a tile ahead; -1 behind the end.
   const int32_t* ld_table = p.table + static_cast<int64_t>(ld.b) * p.max_blocks;
   int ld_pos = ld.tile * S::kTile + warp * S::kTok + tok_lane;
@@ -267,25 +279,28 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       const uint32_t slot = ld_pos - ld_page * p.c.page.d, at = there ? blk : 0;
       const uint32_t in = there ? slot : 0;
       const uint32_t ko = at * p.k_block + in * p.k_token, vo = at * p.v_block + in * p.v_token;
-      const uint32_t mask = __ballot_sync(0xffffffffu, there) >> my_row;      // (lanes 16-31 repeat the tokens of a tile of 16)
-      const uint32_t k_mask = k_there ? mask : 0u, v_mask = v_there ? mask : 0u;
+      const uint32_t mask = __ballot_sync(0xffffffffu, there);
+      const uint32_t at_k = dst + lane_dst, at_v = at_k + S::kHalf;
+      auto to = [&](uint32_t base, int i) { return (base ^ (S::kRow >= 128 ? ((i * kRowsPer) & 7) << 4 : 0)) + i * kRowsPer * S::kRow; };
+      if (__all_sync(0xffffffffu, mask == 0xffffffffu && k_there && v_there)) {
 #pragma unroll
-      for (int i = 0; i < S::kTok / kRowsPer; ++i) {
-        const int r = i * kRowsPer + my_row;
-        const uint32_t o = __shfl_sync(0xffffffffu, ko, r);
-        cp16(dst + swz<S::kRow>(r, my_chunk), kbase + static_cast<uint64_t>(o) * 16, (k_mask >> (i * kRowsPer)) & 1u);
-      }
+        for (int i = 0; i < kIter; ++i) cp16_all(to(at_k, i), kbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, ko, i, kChunks)) * 16, policy);
 #pragma unroll
-      for (int i = 0; i < S::kTok / kRowsPer; ++i) {
-        const int r = i * kRowsPer + my_row;
-        const uint32_t o = __shfl_sync(0xffffffffu, vo, r);
-        cp16(dst + S::kHalf + swz<S::kRow>(r, my_chunk), vbase + static_cast<uint64_t>(o) * 16, (v_mask >> (i * kRowsPer)) & 1u);
+        for (int i = 0; i < kIter; ++i) cp16_all(to(at_v, i), vbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, vo, i, kChunks)) * 16, policy);
+      } else {                                          // zeros for rows behind the end and for values that a row does not have
+        const uint32_t mine = mask >> (my_row * kChunks), k_mask = k_there ? mine : 0u, v_mask = v_there ? mine : 0u;
+#pragma unroll
+        for (int i = 0; i < kIter; ++i)
+          cp16(to(at_k, i), kbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, ko, i, kChunks)) * 16, (k_mask >> i) & 1u, policy);
+#pragma unroll
+        for (int i = 0; i < kIter; ++i)
+          cp16(to(at_v, i), vbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, vo, i, kChunks)) * 16, (v_mask >> i) & 1u, policy);
       }
       if constexpr (kInt8) {
         const uint32_t sc = dst + 2 * S::kHalf + tok_lane * 4;
         const uint32_t kso = at * p.ks_block + in * p.ks_token, vso = at * p.vs_block + in * p.vs_token;
-        if (S::kTok == 32 || lane < 16) cp4(sc, ksbase + static_cast<uint64_t>(kso) * 4, there);
-        if (S::kTok == 32 || lane >= 16) cp4(sc + S::kScale, vsbase + static_cast<uint64_t>(vso) * 4, there);
+        if (S::kTok == 32 || my_chunk < kIter) cp4(sc, ksbase + static_cast<uint64_t>(kso) * 4, there);
+        if (S::kTok == 32 || my_chunk >= kIter) cp4(sc + S::kScale, vsbase + static_cast<uint64_t>(vso) * 4, there);
       }
       --ld.left;
       ld_pos += S::kTile;
@@ -440,8 +455,6 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[g][n][0] = s[g][n][1] = s[g][n][2] = s[g][n][3] = 0.0f;
-#pragma unroll
         for (int c4 = 0; c4 < kSteps; c4 += 4) {        // 64 values of d at a time: what is past D is zero in both
           if (c4 >= k_steps) break;
 #pragma unroll
@@ -455,11 +468,17 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
                 const uint32_t x = r[2 * j] ^ 0x80808080u, y = r[2 * j + 1] ^ 0x80808080u;
                 const uint32_t a[4] = {codes_f16<0, 1>(x), codes_f16<0, 1>(y), codes_f16<2, 3>(x), codes_f16<2, 3>(y)};
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma16<true>(s[g][n], a, q_fragment(c + j, n));
+                for (int n = 0; n < NT; ++n) {
+                  if (c + j == 0) mma16<true, true>(s[g][n], a, q_fragment(0, n));
+                  else mma16<true>(s[g][n], a, q_fragment(c + j, n));
+                }
               }
             } else {
 #pragma unroll
-              for (int n = 0; n < NT; ++n) mma16<false>(s[g][n], r, q_fragment(c, n));
+              for (int n = 0; n < NT; ++n) {
+                if (c == 0) mma16<false, true>(s[g][n], r, q_fragment(0, n));
+                else mma16<false>(s[g][n], r, q_fragment(c, n));
+              }
             }
           }
         }
@@ -471,22 +490,38 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
           k0 = scales[g * 16 + row];
           k1 = scales[g * 16 + row + 8];
         }
-        const bool out0 = pos0 + g * 16 + row >= L, out1 = pos0 + g * 16 + row + 8 >= L;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            s[g][n][e] = out0 ? -INFINITY : s[g][n][e] * (f[n][e] * k0);
-            s[g][n][2 + e] = out1 ? -INFINITY : s[g][n][2 + e] * (f[n][e] * k1);
+            s[g][n][e] *= f[n][e] * k0;
+            s[g][n][2 + e] *= f[n][e] * k1;
           }
         }
-        if (p.weights) {
-          float* dst = score_at + static_cast<int64_t>(tile * S::kTile + g * 16) * p.score_heads;
+      }
+      const int left = L - pos0 - row;                  // tokens from this thread's first one on
+      if (pos0 + S::kTok > L) {                         // (uniform) the sequence ends in this tile
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if (left <= g * 16) s[g][n][e] = -INFINITY;
+              if (left <= g * 16 + 8) s[g][n][2 + e] = -INFINITY;
+            }
+          }
+        }
+      }
+      if (p.weights) {
+        float* dst = score_at + static_cast<int64_t>(tile) * (S::kTile * p.score_heads);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             if (n * 8 + 2 * quad < nh) {
-              if (!out0) *reinterpret_cast<float2*>(dst + n * 8) = make_float2(s[g][n][0], s[g][n][1]);
-              if (!out1) *reinterpret_cast<float2*>(dst + 8 * p.score_heads + n * 8) = make_float2(s[g][n][2], s[g][n][3]);
+              if (left > g * 16) *reinterpret_cast<float2*>(dst + (g * 16) * p.score_heads + n * 8) = make_float2(s[g][n][0], s[g][n][1]);
+              if (left > g * 16 + 8) *reinterpret_cast<float2*>(dst + (g * 16 + 8) * p.score_heads + n * 8) = make_float2(s[g][n][2], s[g][n][3]);
             }
           }
         }
@@ -699,10 +734,16 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 
 // Joins the partial results of cut sequences (CTAs [0, runs x U): the one where the sequence begins), and adds the attention weights
 // (the other CTAs: (sequence, KV head) x share of the positions) from the scores that the first kernel left.
+__device__ __forceinline__ void join_pair(float& m, float& l, float om, float ol) {
+  const float mn = fmaxf(m, om);
+  if (mn != -INFINITY) l = l * ex2(m - mn) + ol * ex2(om - mn);
+  m = mn;
+}
+
 __global__ void __launch_bounds__(kJoinThreads)
 attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
-  __shared__ float f[kMaxSlots * 2];
   __shared__ float4 sums[kJoinThreads];
+  __shared__ float2 mls[kJoinThreads];
   extern __shared__ float lse2_sm[];             // [G]
   pdl_wait_primary();
   pdl_launch_dependents();
@@ -714,70 +755,68 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     if (tail.x < 0) return;
     const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
     const int n = tail.y - run + 1;              // pieces: slot 1 of this CTA, slot 0 of the runs after it
-    auto slot = [&](int i) { return i == 0 ? static_cast<int64_t>(blockIdx.x) * 2 + 1 : (static_cast<int64_t>(run + i) * p.U + unit) * 2; };
-    for (int r = tid >> 5; r < nh; r += kJoinThreads / 32) {       // a warp for each row's maximum and sum
-      float m = -INFINITY, l = 0.0f;
-      for (int i = tid & 31; i < n; i += 32) {
-        const float2 x = *reinterpret_cast<const float2*>(p.part_ml + (slot(i) * p.part_rows + r) * 2);
-        const float mn = fmaxf(m, x.x);
-        if (mn != -INFINITY) l = l * ex2(m - mn) + x.y * ex2(x.x - mn);
-        m = mn;
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, d), ol = __shfl_xor_sync(0xffffffffu, l, d);
-        const float mn = fmaxf(m, om);
-        if (mn != -INFINITY) l = l * ex2(m - mn) + ol * ex2(om - mn);
-        m = mn;
-      }
-      if ((tid & 31) == 0) {
-        f[r] = m == -INFINITY ? 0.0f : m;
-        f[kMaxSlots + r] = 1.0f / l;
-        if (p.lse) p.lse[static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0 + r] = (m + log2f(l)) * 0.6931471805599453f;
-      }
-    }
-    __syncthreads();
-    const int vecs = p.c.Dv / 4, items = nh * vecs;
-    const int share = items >= kJoinThreads ? 1 : kJoinThreads / items;          // threads that split an item's pieces
-    for (int base = 0; base < items; base += kJoinThreads / share) {
-      const int item = base + (tid / share), part = tid % share;
-      const bool on = tid / share < kJoinThreads / share && item < items;
+    const int Dv = p.c.Dv, vecs = Dv / 4, items = nh * vecs;
+    const int share = items >= kJoinThreads ? 1 : kJoinThreads / items, at_once = kJoinThreads / share;      // threads that split an item's pieces
+    const int my = tid / share, part = tid - my * share;
+    const int64_t out0 = static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0;
+    for (int base = 0; base < items; base += at_once) {
+      const int item = base + my;
+      const bool on = my < at_once && item < items;
+      const int r = item / vecs, d = (item - r * vecs) * 4;
       float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (on) {
-        const int r = item / vecs, d = (item - r * vecs) * 4;
+      float m = -INFINITY, l = 0.0f;
+      if (on) {                                  // maximum, sum and output together: one round trip to memory
 #pragma unroll 4
         for (int i = part; i < n; i += share) {
-          const int64_t s = slot(i) * p.part_rows + r;
-          const float w = ex2(p.part_ml[s * 2] - f[r]);
-          const float4 x = *reinterpret_cast<const float4*>(p.part + s * p.c.Dv + d);
-          acc.x = fmaf(x.x, w, acc.x);
-          acc.y = fmaf(x.y, w, acc.y);
-          acc.z = fmaf(x.z, w, acc.z);
-          acc.w = fmaf(x.w, w, acc.w);
+          const int64_t slot = i == 0 ? static_cast<int64_t>(blockIdx.x) * 2 + 1 : (static_cast<int64_t>(run + i) * p.U + unit) * 2;
+          const int64_t s = slot * p.part_rows + r;
+          const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + s * 2);
+          const float4 x = *reinterpret_cast<const float4*>(p.part + s * Dv + d);
+          const float mn = fmaxf(m, ml.x);
+          const float a = m == -INFINITY ? 0.0f : ex2(m - mn), w = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mn);
+          m = mn;
+          l = l * a + ml.y * w;
+          acc.x = acc.x * a + x.x * w;
+          acc.y = acc.y * a + x.y * w;
+          acc.z = acc.z * a + x.z * w;
+          acc.w = acc.w * a + x.w * w;
         }
       }
-      sums[tid] = acc;
-      __syncthreads();
+      if (share > 1) {
+        __syncthreads();
+        sums[tid] = acc;
+        mls[tid] = make_float2(m, l);
+        __syncthreads();
+      }
       if (on && part == 0) {
-        for (int i = 1; i < share; ++i) {
-          const float4 x = sums[tid + i];
-          acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+        if (share > 1) {
+          for (int i = 1; i < share; ++i) m = fmaxf(m, mls[tid + i].x);
+          l = 0.0f;
+          acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int i = 0; i < share; ++i) {
+            const float2 ml = mls[tid + i];
+            const float w = ml.x == -INFINITY ? 0.0f : ex2(ml.x - m);
+            const float4 x = sums[tid + i];
+            l = fmaf(ml.y, w, l);
+            acc.x = fmaf(x.x, w, acc.x);
+            acc.y = fmaf(x.y, w, acc.y);
+            acc.z = fmaf(x.z, w, acc.z);
+            acc.w = fmaf(x.w, w, acc.w);
+          }
         }
-        const int r = item / vecs, d = (item - r * vecs) * 4;
-        const float inv = f[kMaxSlots + r];
-        *reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0 + r) * p.c.Dv + d) =
-            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        const float inv = 1.0f / l;
+        *reinterpret_cast<uint2*>(p.out + (out0 + r) * Dv + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (d == 0 && p.lse) p.lse[out0 + r] = (m + log2f(l)) * 0.6931471805599453f;
       }
-      __syncthreads();
     }
     return;
   }
 
   const int w = blockIdx.x - join_ctas, share = w % p.join_weight_ctas, bk = w / p.join_weight_ctas;
   const int b = bk / p.c.Hkv, hk = bk - b * p.c.Hkv;
+  const int2 span = p.seq_runs[b];               // (anything at all for an empty sequence)
   const int L = seq_len(p, b);
   if (L == 0 || static_cast<int64_t>(share) * kJoinThreads >= L) return;
-  const int2 span = p.seq_runs[b];
   for (int g = tid >> 5; g < p.G; g += kJoinThreads / 32) {
     float lg;
     if (span.x == span.y) {
@@ -788,16 +827,12 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
       for (int i = tid & 31; i <= span.y - span.x; i += 32) {
         const int64_t slot = (static_cast<int64_t>(span.x + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0);
         const float2 x = *reinterpret_cast<const float2*>(p.part_ml + (slot * p.part_rows + r) * 2);
-        const float mn = fmaxf(m, x.x);
-        if (mn != -INFINITY) l = l * ex2(m - mn) + x.y * ex2(x.x - mn);
-        m = mn;
+        join_pair(m, l, x.x, x.y);
       }
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) {
         const float om = __shfl_xor_sync(0xffffffffu, m, d), ol = __shfl_xor_sync(0xffffffffu, l, d);
-        const float mn = fmaxf(m, om);
-        if (mn != -INFINITY) l = l * ex2(m - mn) + ol * ex2(om - mn);
-        m = mn;
+        join_pair(m, l, om, ol);
       }
       lg = m + log2f(l);
     }
@@ -999,7 +1034,7 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.scores = reinterpret_cast<float*>(ws + pl.scores);
   p.part_rows = pl.part_rows;
   // as many CTAs for the weights as fill the machine a few times, none with less than a block of positions
-  const int64_t most = (ld + kJoinThreads - 1) / kJoinThreads, fill = (8LL * sm_count() + static_cast<int64_t>(B) * cache->Hkv - 1) / (static_cast<int64_t>(B) * cache->Hkv);
+  const int64_t most = (ld + kJoinThreads - 1) / kJoinThreads, fill = (4LL * sm_count() + static_cast<int64_t>(B) * cache->Hkv - 1) / (static_cast<int64_t>(B) * cache->Hkv);
   p.join_weight_ctas = static_cast<int>(most < fill ? (most < 1 ? 1 : most) : fill);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return with_shape(int8, widest, slots, Launch{p, s});

@@ -856,7 +856,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
       float4 x[kAtOnce];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i)
-        if (i < n) x[i] = __ldcs(reinterpret_cast<const float4*>(s + i * score_step));
+        if (i < n) x[i] = __ldcg(reinterpret_cast<const float4*>(s + i * score_step));
       const float l0 = lse2_sm[0], l1 = lse2_sm[1], l2 = lse2_sm[2], l3 = p.G > 3 ? lse2_sm[3] : INFINITY;
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i)
@@ -867,7 +867,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
         float2 x[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
-          if (i < n) x[i] = __ldcs(reinterpret_cast<const float2*>(s + i * score_step + g));
+          if (i < n) x[i] = __ldcg(reinterpret_cast<const float2*>(s + i * score_step + g));
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i)
           if (i < n) acc[i] += ex2(x[i].x - l0) + (l1 != INFINITY ? ex2(x[i].y - l1) : 0.0f);

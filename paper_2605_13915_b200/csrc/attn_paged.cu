@@ -57,7 +57,7 @@ struct PagedAttnParams {
   // workspace
   float* part;                // [CTA][2][rows][Dv]: unnormalised outputs
   float* part_ml;             // [CTA][2][rows][2]: maximum (log2) and sum
-  int2* tail;                 // [CTA] what the join does for it: {sequence cut at the end of its run or -1, last run of that sequence}
+  int4* tail;                 // [CTA] {sequence cut at the end of its run or -1, first and last run of that sequence}
   int2* seq_runs;             // [B] {first, last run}
   float* lse2;                // [B, Hq] log2-sum of uncut sequences
   float* scores;              // [B, Hkv, score_ld, score_heads] log2 scores
@@ -204,7 +204,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   }
   const int T = __shfl_sync(0xffffffffu, before, 31);
   before -= mine;
-  if (threadIdx.x == 0) p.tail[blockIdx.x] = make_int2(-1, 0);
+  if (threadIdx.x == 0) p.tail[blockIdx.x] = make_int4(-1, 0, 0, 0);
   const int runs = min(p.runs, T);                // (no empty runs)
   if (run >= runs) return;
   auto run_start = [&](int r) { return static_cast<int>(static_cast<int64_t>(r) * T / runs); };
@@ -719,20 +719,17 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       }
       __syncthreads();
     }
-    if (from_start && unit == 0 && threadIdx.x == 0) {
-      const int64_t at = first + (static_cast<int64_t>(end - first) - cur.left - seg);      // the sequence's first tile in the list
-      const int64_t last = at + (L + S::kTile - 1) / S::kTile - 1;
-      p.seq_runs[b] = make_int2(run, static_cast<int>(((last + 1) * runs - 1) / T));
-    }
-    if (from_start && !to_end && threadIdx.x == 0) {
-      const int64_t last = static_cast<int64_t>(end) + (L + S::kTile - 1) / S::kTile - seg - 1;
-      p.tail[blockIdx.x] = make_int2(b, static_cast<int>(((last + 1) * runs - 1) / T));
+    if (threadIdx.x == 0) {                      // the runs that have tiles of this sequence
+      const int64_t at = static_cast<int64_t>(end) - cur.left - seg - seg_first, upto = at + (L + S::kTile - 1) / S::kTile;
+      const int run0 = static_cast<int>(((at + 1) * runs - 1) / T), run1 = static_cast<int>((upto * runs - 1) / T);
+      if (from_start && unit == 0) p.seq_runs[b] = make_int2(run0, run1);
+      if (!to_end) p.tail[blockIdx.x] = make_int4(b, run0, run1, 0);
     }
   }
   cp_wait<0>();
 }
 
-// Joins the partial results of cut sequences (CTAs [0, runs x U): the one where the sequence begins), and adds the attention weights
+// Joins the partial results of cut sequences (CTAs [0, runs x U), those whose run ends inside one), and adds the attention weights
 // (the other CTAs: (sequence, KV head) x share of the positions) from the scores that the first kernel left.
 __device__ __forceinline__ void join_pair(float& m, float& l, float om, float ol) {
   const float mn = fmaxf(m, om);
@@ -751,35 +748,50 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
   const int tid = threadIdx.x;
   if (static_cast<int>(blockIdx.x) < join_ctas) {
     const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
-    const int2 tail = p.tail[blockIdx.x];
+    const int4 tail = p.tail[blockIdx.x];
     if (tail.x < 0) return;
+    // The CTAs of all runs but the last one that have tiles of this sequence share the join: each takes some of the outputs, four values of
+    // a head an item, and some threads an item, which take some of the pieces (slot 1 of the first run, slot 0 of the others).
     const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
-    const int n = tail.y - run + 1;              // pieces: slot 1 of this CTA, slot 0 of the runs after it
-    const int Dv = p.c.Dv, vecs = Dv / 4, items = nh * vecs;
-    const int share = items >= kJoinThreads ? 1 : kJoinThreads / items, at_once = kJoinThreads / share;      // threads that split an item's pieces
+    const int n = tail.z - tail.y + 1, helpers = n - 1, helper = run - tail.y;
+    const int Dv = p.c.Dv, vecs = Dv / 4, all = nh * vecs;
+    const int item0 = all * helper / helpers, items = all * (helper + 1) / helpers - item0;
+    if (items == 0) return;
+    const int share = items >= kJoinThreads ? 1 : min(min(kJoinThreads / items, 16), n), at_once = kJoinThreads / share;
     const int my = tid / share, part = tid - my * share;
     const int64_t out0 = static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0;
     for (int base = 0; base < items; base += at_once) {
-      const int item = base + my;
-      const bool on = my < at_once && item < items;
-      const int r = item / vecs, d = (item - r * vecs) * 4;
+      const bool on = my < at_once && base + my < items;
+      const int item = item0 + base + my, r = item / vecs, d = (item - r * vecs) * 4;
       float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       float m = -INFINITY, l = 0.0f;
-      if (on) {                                  // maximum, sum and output together: one round trip to memory
-#pragma unroll 4
-        for (int i = part; i < n; i += share) {
-          const int64_t slot = i == 0 ? static_cast<int64_t>(blockIdx.x) * 2 + 1 : (static_cast<int64_t>(run + i) * p.U + unit) * 2;
-          const int64_t s = slot * p.part_rows + r;
-          const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + s * 2);
-          const float4 x = *reinterpret_cast<const float4*>(p.part + s * Dv + d);
-          const float mn = fmaxf(m, ml.x);
-          const float a = m == -INFINITY ? 0.0f : ex2(m - mn), w = ml.x == -INFINITY ? 0.0f : ex2(ml.x - mn);
-          m = mn;
-          l = l * a + ml.y * w;
-          acc.x = acc.x * a + x.x * w;
-          acc.y = acc.y * a + x.y * w;
-          acc.z = acc.z * a + x.z * w;
-          acc.w = acc.w * a + x.w * w;
+      if (on) {                                  // maximum, sum and output together: one round trip to memory for four pieces
+        constexpr int kPieces = 4;
+        for (int i0 = part; i0 < n; i0 += share * kPieces) {
+          float2 ml[kPieces];
+          float4 x[kPieces];
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) {
+            const int i = i0 + k * share;
+            if (i < n) {
+              const int64_t s = ((static_cast<int64_t>(tail.y + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + r;
+              ml[k] = *reinterpret_cast<const float2*>(p.part_ml + s * 2);
+              x[k] = *reinterpret_cast<const float4*>(p.part + s * Dv + d);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) {
+            if (i0 + k * share < n) {
+              const float mn = fmaxf(m, ml[k].x);
+              const float a = m == -INFINITY ? 0.0f : ex2(m - mn), w = ml[k].x == -INFINITY ? 0.0f : ex2(ml[k].x - mn);
+              m = mn;
+              l = l * a + ml[k].y * w;
+              acc.x = acc.x * a + x[k].x * w;
+              acc.y = acc.y * a + x[k].y * w;
+              acc.z = acc.z * a + x[k].z * w;
+              acc.w = acc.w * a + x[k].w * w;
+            }
+          }
         }
       }
       if (share > 1) {
@@ -904,7 +916,7 @@ bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, Pag
   };
   pl->part = take(ctas * 2 * pl->part_rows * Dv * 4);
   pl->ml = take(ctas * 2 * pl->part_rows * 8);
-  pl->tail = take(ctas * sizeof(int2));
+  pl->tail = take(ctas * sizeof(int4));
   pl->seq_runs = take(static_cast<size_t>(B) * sizeof(int2));
   pl->lse2 = take(static_cast<size_t>(B) * Hq * 4);
   pl->scores = take(static_cast<size_t>(B) * Hkv * ld * pl->score_heads * 4);
@@ -1032,7 +1044,7 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.slots = pl.slots;
   p.part = reinterpret_cast<float*>(ws + pl.part);
   p.part_ml = reinterpret_cast<float*>(ws + pl.ml);
-  p.tail = reinterpret_cast<int2*>(ws + pl.tail);
+  p.tail = reinterpret_cast<int4*>(ws + pl.tail);
   p.seq_runs = reinterpret_cast<int2*>(ws + pl.seq_runs);
   p.lse2 = reinterpret_cast<float*>(ws + pl.lse2);
   p.scores = reinterpret_cast<float*>(ws + pl.scores);

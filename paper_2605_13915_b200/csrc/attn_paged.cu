@@ -30,8 +30,6 @@ namespace msd {
 
 namespace {
 
-constexpr int kPWarps = 4;
-constexpr int kPThreads = 32 * kPWarps;
 constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
 constexpr float kHeld = 8.0f;               // how far (log2) a score may exceed its reference before that moves
@@ -130,23 +128,25 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
 // keys and values; the rings of all CTAs of an SM together hold about 200 KB.
 template <bool kInt8, int DP, int kHeads>
 struct Shape {
+  static constexpr int kWarps = !kInt8 && DP == 256 ? 6 : 4;
+  static constexpr int kThreads = 32 * kWarps;
   static constexpr int kEs = kInt8 ? 1 : 2;
-  static constexpr int kTok = kInt8 && DP <= 128 ? 32 : 16;
+  static constexpr int kTok = DP == 64 || (kInt8 && DP == 128) ? 32 : 16;
   static constexpr int kRow = DP * kEs;                         // bytes of a row in shared memory
   static constexpr int kHalf = kTok * kRow;                     // keys, then values
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
   static constexpr bool kWide = kHalf >= 4096;                  // 8 KB a tile and more
-  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (DP == 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
-  static constexpr int kStages = kWide ? (kCtasPerSm == 3 ? 2 : 3) : (kHeads == 8 ? 3 : 4);
+  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (DP <= 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
+  static constexpr int kStages = kWide ? (kCtasPerSm == 3 || kHalf >= 8192 ? 2 : 3) : (kHeads == 8 ? 3 : 4);
   static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
-  static constexpr int kRing = kPWarps * kStages * kStage;
+  static constexpr int kRing = kWarps * kStages * kStage;
   // The warps' outputs meet in the stages that their last tiles left, all heads or 8 at a time; rows four words apart in the banks
   // where there is room for that.
   static constexpr int kMeet = kHeads * DP * 4 <= kStage ? kHeads : 8;
   static constexpr int kORow = kMeet * (DP + 4) * 4 <= kStage ? DP + 4 : DP;
   static constexpr int kSmem = kRing + (kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0);
-  static constexpr int kTile = kPWarps * kTok;                  // tokens of a CTA's tile
+  static constexpr int kTile = kWarps * kTok;                  // tokens of a CTA's tile
   static_assert(kMeet * kORow * 4 <= kStage, "a stage has to hold a warp's outputs");
   static_assert(kCtasPerSm * (kSmem + 2304) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
 };
@@ -163,12 +163,12 @@ __device__ __forceinline__ int seq_len(const PagedAttnParams& p, int b) {
 }
 
 template <bool kInt8, int DP, int kHeads>
-__global__ void __launch_bounds__(kPThreads, (Shape<kInt8, DP, kHeads>::kCtasPerSm))
+__global__ void __launch_bounds__((Shape<kInt8, DP, kHeads>::kThreads), (Shape<kInt8, DP, kHeads>::kCtasPerSm))
 attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   using S = Shape<kInt8, DP, kHeads>;
   constexpr int NT = kHeads / 8;                        // column tiles of heads
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ float ml[3][kPWarps][kHeads];              // of a warp: references, sums, units of its outputs
+  __shared__ float ml[3][S::kWarps][kHeads];              // of a warp: references, sums, units of its outputs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
   const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kHeads;        // first head of the group within the KV head
@@ -384,7 +384,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       }
     };
     if constexpr (S::kQInSmem) {
-      for (int s = warp; s < kSteps; s += kPWarps) {
+      for (int s = warp; s < kSteps; s += S::kWarps) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) sm_q[(s * NT + n) * 32 + lane] = fragment(raw_q(s, n), n);
       }
@@ -683,15 +683,15 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       __syncthreads();
       const float* met = reinterpret_cast<const float*>(smem + (fill_u - ring_u));      // warp 0's; the next one's is a ring further
       const int heads = min(nh - pass * S::kMeet, S::kMeet);
-      for (int i = threadIdx.x; i < heads * vecs; i += kPThreads) {
+      for (int i = threadIdx.x; i < heads * vecs; i += S::kThreads) {
         const int hl = i / vecs, d = (i - hl * vecs) * 4, h = pass * S::kMeet + hl;
         float mh = ml[0][0][h];
 #pragma unroll
-        for (int w = 1; w < kPWarps; ++w) mh = fmaxf(mh, ml[0][w][h]);
+        for (int w = 1; w < S::kWarps; ++w) mh = fmaxf(mh, ml[0][w][h]);
         float lh = 0.0f;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < kPWarps; ++w) {              // (a fixed order)
+        for (int w = 0; w < S::kWarps; ++w) {              // (a fixed order)
           const float mw = ml[0][w][h];
           if (mw != -INFINITY) {
             const float r = ex2(mw - mh), u = kInt8 ? r * ml[2][w][h] : r;
@@ -931,7 +931,7 @@ msd_status_t launch_paged(const PagedAttnParams& p, cudaStream_t s) {
   static DeviceOnce once;
   if (!once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem) == cudaSuccess; })) return MSD_ERR_CUDA;
   const bool pdl = option(OPT_NO_PDL) != 1;
-  if (launch_pdl(kernel, dim3(p.runs * p.U), dim3(kPThreads), Sh::kSmem, s, pdl, p) != cudaSuccess) {
+  if (launch_pdl(kernel, dim3(p.runs * p.U), dim3(Sh::kThreads), Sh::kSmem, s, pdl, p) != cudaSuccess) {
     cudaGetLastError();
     return MSD_ERR_CUDA;
   }

@@ -235,11 +235,12 @@ constexpr int kBins = 2048, kPasses = 3;
 constexpr uint32_t kNowhere = 0xFFFFFFFFu;
 
 template <int kKeys, int kSelThreads>        // keys a thread keeps; 0: none, they are read from memory in every pass
-__global__ void __launch_bounds__(kSelThreads, 1024 / kSelThreads)
-kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
+__global__ void __launch_bounds__(kSelThreads, kSelThreads == 128 ? 6 : 1024 / kSelThreads)
+kv_evict_select_kernel(const __grid_constant__ EvictParams p, int cluster_ctas) {
+  const int ctas = kSelThreads > 128 ? cluster_ctas : 1;
   constexpr int kSelWarps = kSelThreads / 32, kBinsEach = kBins / kSelThreads;
   __shared__ __align__(16) uint32_t own[kBins];          // histogram of this CTA's keys
-  __shared__ __align__(16) uint32_t all[kPasses][kBins]; // of the cluster's, a pass each
+  __shared__ __align__(16) uint32_t all[kSelThreads > 128 ? kPasses : 1][kSelThreads > 128 ? kBins : 1];      // of the cluster's, a pass each (128 threads: no cluster)
   __shared__ uint32_t range[2];                         // smallest and largest key of this CTA
   __shared__ uint32_t part[kSelWarps][2];
   __shared__ uint32_t found[3];                         // bin, keys above it, keys in it
@@ -303,7 +304,7 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
     smallest = __reduce_min_sync(0xffffffffu, smallest);
     largest = __reduce_max_sync(0xffffffffu, largest);
     if (lane == 0) { part[warp][0] = smallest; part[warp][1] = largest; }
-    if (ctas > 1) {
+    if (kSelThreads > 128 && ctas > 1) {
       for (int i = threadIdx.x; i < kPasses * kBins; i += kSelThreads) (&all[0][0])[i] = 0;
     }
     __syncthreads();
@@ -334,7 +335,7 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int ctas) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kBinsEach; ++i) c[i] = own[threadIdx.x * kBinsEach + i];
-      if (ctas > 1) {
+      if (kSelThreads > 128 && ctas > 1) {
 #pragma unroll
         for (int i = 0; i < kBinsEach; ++i) {
           if (c[i] == 0) continue;
@@ -632,7 +633,8 @@ msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* b
   int ctas = 1;
   while (ctas < 8 && (p.cap > ctas * 16384LL || (p.cap > ctas * 2048LL && units * ctas <= sm_count()))) ctas *= 2;
   const int64_t keys = (p.cap + ctas * 512LL - 1) / (ctas * 512LL);
-  const cudaError_t err = keys <= 4    ? launch_select<4, 512>(p, units, ctas, s, pdl)
+  const cudaError_t err = p.cap <= 512   ? launch_select<4, 128>(p, units, 1, s, pdl)
+                          : keys <= 4  ? launch_select<4, 512>(p, units, ctas, s, pdl)
                           : keys <= 8  ? launch_select<8, 512>(p, units, ctas, s, pdl)
                           : keys <= 16 ? launch_select<16, 512>(p, units, ctas, s, pdl)
                           : keys <= 32 ? launch_select<16, 1024>(p, units, ctas, s, pdl)

@@ -98,6 +98,47 @@ def test_attention_of_many_short_sequences(int8):
     _check_attention(q, c, 0.125, out, lse, before, weights)
 
 
+def test_attention_with_more_heads_than_places_on_the_machine():
+    """Every CTA walks all sequences of its KV head; one query head each, and 8 groups of 16 for the others."""
+    for Hq, Hkv in ((900, 900), (640, 5)):
+        c = make_cache([70, 0, 33, 130], Hkv, 16, 16, 16, int8=True, seed=2)
+        q = torch.randn(4, Hq, 16, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+        before = torch.rand(4, Hkv, 130, generator=torch.Generator().manual_seed(3)).cuda()
+        weights = before.clone()
+        out, lse = binding.attn_decode_paged(q, *_args(c), 0.25, weights=weights, want_lse=True)
+        binding.last_device_status()
+        _check_attention(q, c, 0.25, out, lse, before, weights)
+
+
+def test_attention_over_a_cache_in_one_piece():
+    """A page that holds everything: the contiguous cache of one sequence, and one page of two that share it as a prefix."""
+    c = make_cache([3000], 2, 64, 64, 5000, seed=14)
+    q = torch.randn(1, 8, 64, generator=torch.Generator().manual_seed(14)).to(torch.bfloat16).cuda()
+    _check_attention(q, c, 0.125, binding.attn_decode_paged(q, *_args(c), 0.125))
+    c["table"], c["seqlens"] = c["table"].expand(2, 1).contiguous(), torch.tensor([3000, 1700], dtype=torch.int32, device="cuda")
+    q = q.expand(2, 8, 64).contiguous()
+    before = torch.zeros(2, 2, 3000, device="cuda")
+    weights = before.clone()
+    out = binding.attn_decode_paged(q, *_args(c), 0.125, weights=weights)
+    binding.last_device_status()
+    _check_attention(q, c, 0.125, out, None, before, weights)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_attention_does_not_look_at_other_places(int8):
+    """What lies behind the last token, in pages of nobody and in the workspace, is poison in the other tests; here the table's unused
+    entries point at pages that do not exist, and values of one sequence are huge."""
+    c = make_cache([50, 77], 2, 64, 64, 16, int8, seed=15)
+    wide = torch.full((2, 9), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    wide[:, :5] = torch.where(c["table"] >= 0, c["table"], 2 ** 31 - 1)
+    q = torch.randn(2, 4, 64, generator=torch.Generator().manual_seed(15)).to(torch.bfloat16).cuda()
+    q[1] *= 1e30
+    want = binding.attn_decode_paged(q[:1], c["k"], c["v"], c["k_scale"], c["v_scale"], c["table"][:1], c["seqlens"][:1], 0.125)
+    got = binding.attn_decode_paged(q, c["k"], c["v"], c["k_scale"], c["v_scale"], wide, c["seqlens"], 0.125)
+    binding.last_device_status()
+    assert torch.equal(got[:1], want)
+
+
 def test_attention_of_nothing_but_empty_sequences():
     c = make_cache([0, 0, 0], 2, 128, 128, 16)
     q = torch.ones(3, 8, 128, dtype=torch.bfloat16, device="cuda")
@@ -415,6 +456,40 @@ def test_eviction_reports_what_does_not_fit():
     reported(c["table"], torch.tensor([100, 113], dtype=torch.int32, device="cuda"), dst, torch.rand(2, 1, 200, device="cuda"))
     reported(c["table"], c["seqlens"], dst[:, :1].contiguous())                # no room for 40 tokens
     reported(c["table"], c["seqlens"], dst, w[..., :50].contiguous())          # weights of fewer positions
+
+
+# ---- what the wrappers refuse ------------------------------------------------------------------------------------------------
+def test_wrappers_refuse_tensors_that_do_not_fit():
+    c = make_cache([40, 9], 2, 64, 64, 16, seed=1, poison=False)
+    i = make_cache([40, 9], 2, 64, 64, 16, int8=True, seed=1, poison=False)
+    k, v, _, _, table, n = _args(c)
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")
+    q, cu, new = z(2, 4, 64), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), z(2, 2, 64)
+    w = z(2, 2, 64, dtype=torch.float32)
+    attend = lambda q=q, k=k, v=v, ks=None, vs=None, t=table, n=n, **more: binding.attn_decode_paged(q, k, v, ks, vs, t, n, 0.1, **more)
+    append = lambda a=new, b=new, t=table, n=n, cu=cu, w=None: binding.kv_append_paged(a, b, k, v, None, None, t, n, cu, weights=w)
+    dst = z(2, 1, dtype=torch.int32)
+    evict = lambda w=w, budget=8, dst=dst, **more: binding.kv_evict_paged(k, v, None, None, table, n, w, budget, dst, **more)
+    for call in (lambda: attend(q=q.float()), lambda: attend(k=k.half(), v=v.half()), lambda: attend(n=n.long()), lambda: attend(t=table.long()),
+                 lambda: attend(v=i["v"]), lambda: attend(weights=w.double()), lambda: append(a=new.float()), lambda: append(cu=cu.float()),
+                 lambda: evict(w=w.to(torch.bfloat16)), lambda: evict(kept=z(2, 2, 8, dtype=torch.int64))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: attend(q=z(2, 4, 128)), lambda: attend(q=z(3, 4, 64)), lambda: attend(q=q.transpose(1, 2).contiguous().transpose(1, 2)),
+                 lambda: attend(k=k.flatten(0, 1)), lambda: attend(v=v[:, :8]), lambda: attend(k=k.transpose(2, 3), v=v.transpose(2, 3)),
+                 lambda: attend(ks=i["k_scale"], vs=i["v_scale"]), lambda: attend(k=i["k"], v=i["v"]), lambda: attend(k=i["k"], v=i["v"], ks=i["k_scale"]),
+                 lambda: attend(t=table[:1]), lambda: attend(n=n[:1]), lambda: attend(t=table.t().contiguous().t()), lambda: attend(weights=z(2, 4, 64, dtype=torch.float32)),
+                 lambda: attend(out=z(2, 4, 32)), lambda: attend(n=n.cpu()), lambda: append(a=z(3, 2, 64)), lambda: append(b=z(2, 2, 32)),
+                 lambda: append(cu=cu[:2]), lambda: append(w=z(2, 1, 64, dtype=torch.float32)), lambda: evict(budget=0), lambda: evict(recent=9),
+                 lambda: evict(sinks=-1), lambda: evict(dst=z(1, 1, dtype=torch.int32)), lambda: evict(kept=z(2, 2, 9, dtype=torch.int32)),
+                 lambda: evict(new_weights=z(2, 1, 64, dtype=torch.float32))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: attend(q=z(2, 3, 64)), lambda: attend(ws=z(4096, dtype=torch.uint8)), lambda: attend(q=z(1, 4, 64).expand(2, 4, 64)),
+                 lambda: evict(recent=5, sinks=4), lambda: evict(dst=table), lambda: evict(new_weights=z(2, 2, 7, dtype=torch.float32))):
+        with pytest.raises(binding.MsdError):
+            call()
+    binding.last_device_status()
 
 
 # ---- together ------------------------------------------------------------------------------------------------------------------

@@ -432,15 +432,16 @@ msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16,
 /*
  * Attention of one new token per sequence over a paged cache, split over the cache's length and joined:
  *   S_hj = softmax_scale * q_h . k_j,  P_h = softmax over the seqlens[b] tokens,  out_h = sum_j P_hj v_j,
- * query head h reading KV head h / (Hq / Hkv).  Products of BF16 values (INT8 codes are exact in BF16; their scales are applied in FP32)
- * with FP32 sums; softmax in FP32; P rounded to BF16 for the product with v.  No decomposition: this is the cache read as it is,
- * beside msd_attn_decode_int8kv_paged, which splits q and P into INT8 components.
+ * query head h reading KV head h / (Hq / Hkv).  q and k are multiplied exactly (INT8 codes in FP16, q scaled by a power of two beside
+ * them; the scales are applied in FP32) and summed in FP32; softmax in FP32; for the product with v, P is the sum of two BF16 values, with INT8
+ * codes P times the value's scale is one FP16 value: 11 bits down to 2^-21 of the largest scale so far, off by 2^-32 of that below.
+ * No decomposition: this is the cache read as it is, beside msd_attn_decode_int8kv_paged, which splits q and P into INT8 components.
  *   q_bf16 [B, Hq, D], rows of a sequence q_ld elements apart (a multiple of 8); out_bf16 [B, Hq, Dv]; lse nullable [B, Hq] FP32
  *   (natural-log sum of exp of the scaled scores).  Hq % Hkv == 0.  Empty sequences give zeros and lse = -inf.
  *   weights nullable [B, Hkv, ld] FP32: weights[b][k][j] += the sum of P_hj over the heads h of KV head k, for j < seqlens[b]; the
  *   rest is left as it is.  ld >= every length.  The sums have a fixed order: equal inputs give equal bits.
- * workspace: >= msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld) bytes (ld = 0 without weights), 1024-byte aligned, no
- * initialisation needed.  Two kernels; nothing is kept from call to call.  The rows of k and of v may spread over 64 GiB each, the scales
+ * workspace: >= msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld) bytes (ld = 0 without weights; with them it holds a score of every
+ * head and position, about 4 B Hq ld bytes), 1024-byte aligned, no initialisation needed.  Two kernels; nothing is kept from call to call.  The rows of k and of v may spread over 64 GiB each, the scales
  * over 16 GiB (more: MSD_ERR_UNSUPPORTED).
  */
 size_t msd_attn_decode_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Dv, int64_t ld);

@@ -4,20 +4,32 @@
 //   S_hj = scale q_h.k_j,  P = softmax(S),  out = P V,  weights_j += sum_h P_hj
 //
 // Bound: HBM.  A token of a KV head is 2 (D + Dv) bytes (BF16) for 2 G (D + Dv) multiply-adds of its G query heads.  An SM takes in
-// 44 bytes a nanosecond, 23 a clock, and the warp-level MMAs of that (16 head slots, used or not) are a fifth of what the pipe does,
+// 44 bytes a nanosecond, 23 a clock, and the warp-level MMAs of that (8 or 16 head slots, used or not) are a fifth of what the pipe does,
 // so nothing here waits for the tensor cores, and what counts is that loads never stop.  Hence no roles and no hand-offs: each warp
 // keeps a ring of token tiles of its own in flight (cp.async, a row's page looked up a tile ahead), multiplies a tile against the
-// query fragments in its registers, keeps its own running maximum, sum and output, and meets the other warps of its CTA only
-// when a sequence ends.
+// query fragments in its registers, keeps its own references, sums and outputs, and meets the other warps of its CTA only when
+// a sequence ends.  32 sequences of 2048 to 8192 tokens, 32 / 8 heads of 128, pages of 16, no weights: BF16 106 us (6.3 TB/s, 0.98 of a plain
+// copy), INT8 67 (5.2 TB/s; 60 of them are the loads alone).  The kernels of this library whose tiles go through tensor memory
+// (tcgen05, a CTA's warps in roles), same box: BF16 without pages 124, INT8 with q and P decomposed 72; 16 query heads a KV head INT8 87 / 161;
+// 8 x 32768 INT8 97 / 96.  With more than 8 slots, or INT8, instructions start to count: 128 / 8 heads BF16 118 us.
 //
-// Fragments (mma m16n8k16): heads are the 16 rows; the scores of 8 tokens are a C fragment, which is the A fragment of the product
-// with v as it stands.  INT8 codes go from shared memory to registers as bytes and become BF16 pairs there (exact): a byte x is
-// (128 + (x & 127)) - (128 + (x & 128)), two byte permutes, masks and one packed subtraction for a pair.
+// Fragments (mma m16n8k16): 16 tokens are the rows and 8 heads the columns, so that up to 8 heads waste nothing.  The scores are a C
+// fragment; transposed in registers (movmatrix) it is the column fragment of the product of v^T (rows: 16 values of d) with P.  INT8
+// codes go from shared memory to registers as bytes and become FP16 pairs there (exact): 1024 + (x + 128) has the byte as its lowest bits, and
+// 1152 is taken off, 5 instructions for 4 values (BF16 pairs, sign and magnitude apart: 8).
+//
+// Precision: q and k (codes) are multiplied exactly and summed in FP32; the sums' error is what an FP32 product has.  P for the
+// product with v is two BF16 values, or one FP16 value with 11 bits for codes; one BF16 value made the result's error 1.4 times that of
+// its own rounding to BF16.
 //
 // Split over the length: the tiles of all sequences form one list, cut into equal runs; run i is walked by U = KV heads x head groups
 // CTAs side by side, one per unit, so that CTAs that run together read neighbouring rows.  The grid is what is resident at once.
 // A sequence inside one run is finished there; only the first and the last of a run can be cut, so a CTA leaves at most two
 // partial results, whatever the lengths are, and a second kernel joins those and turns the scores into weights.
+//
+// Tried and dropped: the last CTA to leave a partial result of a sequence joins them (registers of the tile loop; 32 x 2048-8192
+// tokens 122 -> 124 us at best, one of 1001 10.1 -> 9.0); keys and values asked for one by one as soon as their halves of a stage are free
+// (more in flight, 122 -> 127, 2 x 100000-131072 164 -> 172); scores kept in L2 by a cache hint (0.5 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -57,7 +69,7 @@ struct PagedAttnParams {
   float* part_ml;             // [CTA][2][rows][2]: maximum (log2) and sum
   int4* tail;                 // [CTA] {sequence cut at the end of its run or -1, first and last run of that sequence}
   int2* seq_runs;             // [B] {first, last run}
-  float* lse2;                // [B, Hq] log2-sum of uncut sequences
+  float* lse2;                // [B, Hq] log2-sum of uncut sequences' scores
   float* scores;              // [B, Hkv, score_ld, score_heads] log2 scores
   int part_rows;              // rows of a partial result: min(G, slots)
   int join_weight_ctas;       // CTAs of the join per (sequence, KV head)
@@ -125,7 +137,8 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
 }
 
 // DP: D and Dv rounded up to 64, 128 or 256; kHeads: head slots of a CTA, 8 or 16.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB of
-// keys and values; the rings of all CTAs of an SM together hold about 200 KB.
+// keys and values; the rings of all CTAs of an SM together hold about 200 KB, and more warps with two stages were better than fewer
+// with three (heads of 128, 32 x 2048-8192 tokens: INT8 81 / 85 us, 16 / 16 heads of 80 52 / 57; heads of 64 BF16 60 / 63).
 template <bool kInt8, int DP, int kHeads>
 struct Shape {
   static constexpr int kWarps = !kInt8 && DP == 256 ? 6 : 4;

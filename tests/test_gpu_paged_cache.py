@@ -160,6 +160,23 @@ def test_attention_with_scores_far_apart(int8):
     _check_attention(q, c, 1.0, out, lse, before, weights)
 
 
+def test_attention_with_unequal_scales():
+    """Values whose scales are a million times apart.  P times the scale is FP16 in units of the largest scale: below 2^-21 of it the
+    error is 2^-32 of that scale (rounded up to a power of two) for each token, times its code."""
+    c = make_cache([700, 90], 2, 64, 64, 16, int8=True, seed=16, poison=False)
+    g = torch.Generator().manual_seed(16)
+    c["v_scale"] *= torch.exp2(torch.randint(-10, 11, c["v_scale"].shape, generator=g)).cuda()
+    c["k_scale"] *= torch.exp2(torch.randint(-4, 1, c["k_scale"].shape, generator=g)).cuda()
+    q = torch.randn(2, 8, 64, generator=g).to(torch.bfloat16).cuda()
+    out = binding.attn_decode_paged(q, *_args(c), 0.125)
+    binding.last_device_status()
+    want, _, _, mass, reach = attention(q, c, 0.125)
+    rel = torch.expm1(2 * (64 + 8) * FP32 * reach) + (16 + 700 / 64 + 64) * FP32
+    small = 2.0 ** -32 * 2 * float(c["v_scale"].max()) * 127 * 700
+    bound = HALF_BF16 * want.abs() + (2.0 ** -11 + rel[..., None]) * mass * (1 + 2 * HALF_BF16) + small
+    assert ((out.double() - want).abs() <= bound).all()
+
+
 def test_attention_takes_slices_of_a_projection():
     """q as a slice of a fused projection's result, on another stream than the default one."""
     c = make_cache([130, 40], 2, 64, 64, 16, seed=3)

@@ -225,7 +225,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   const bool here = first >= before && first < before + mine;       // of one lane
   int b_first = b_lo, t_first = first - before;
   if (here) {
-    for (;; ++b_first) {
+    for (; b_first + 1 < b_hi; ++b_first) {
       const int t = (seq_len(p, b_first) + S::kTile - 1) / S::kTile;
       if (t_first < t) break;
       t_first -= t;
@@ -247,9 +247,10 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   ld.left = end - first;
   Walk cur = ld;
   auto next_sequence = [&](Walk& w) {
-    do {
-      w.L = seq_len(p, ++w.b);
-    } while (w.L == 0);
+    do {                                      // (there is one, unless the lengths are changed meanwhile)
+      w.b = min(w.b + 1, p.B - 1);
+      w.L = seq_len(p, w.b);
+    } while (w.L == 0 && w.b + 1 < p.B);
     w.tile = 0;
     w.tiles = (w.L + S::kTile - 1) / S::kTile;
   };

@@ -425,7 +425,9 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int cluster_ctas) 
     const uint32_t pa = a + __popc(ms & lanes_below(lane)), pe = e + __popc(me & lanes_below(lane));
     a += __popc(ms);
     e += __popc(me);
-    return ((ms >> lane) & 1u) || (((me >> lane) & 1u) && pe < need) ? pa + min(pe, need) : kNowhere;
+    const uint32_t at = pa + min(pe, need);
+    // (below the budget as long as the weights are not changed meanwhile; if they are, nothing outside is written all the same)
+    return (((ms >> lane) & 1u) || (((me >> lane) & 1u) && pe < need)) && at < want ? at : kNowhere;
   };
   if constexpr (kKeys > 0) {
     float x[kKeys];
@@ -458,9 +460,10 @@ cudaError_t launch_select(const EvictParams& p, int64_t units, int ctas, cudaStr
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Eviction, second kernel: the kept rows go to their new pages.  Bound: HBM (32 x 8 rows of 2048 INT8 tokens, 281 MB: 49 us, 5.8 TB/s).  A warp takes up to 32 rows: each lane looks up where one of
-// them is and where it goes, and moves its scales; then kLanes lanes (a power of two) copy a row's key and value, 16 bytes at a time,
-// several rows under way.  Sources and destinations never overlap, so the order of the copies does not matter.
+// Eviction, second kernel: the kept rows go to their new pages.  Bound: HBM (32 x 8 rows of 2048 INT8 tokens, 281 MB: 49 us, 5.8 TB/s).
+// A warp takes up to 32 rows: each lane looks up where one of them is and where it goes, and moves its scales; then kLanes lanes (a power of
+// two) copy a row's key and value, 16 bytes at a time, several rows under way.  Sources and destinations never overlap, so the
+// order of the copies does not matter.
 // ---------------------------------------------------------------------------------------------------------------------------
 constexpr int kMoveThreads = 128;
 
@@ -485,8 +488,9 @@ kv_evict_move_kernel(const __grid_constant__ EvictParams p) {
   if (lane < rows) {
     const int i = static_cast<int>(row0) + lane;
     const int32_t from = p.kept[(static_cast<int64_t>(b) * p.c.Hkv + hk) * p.budget + i];
-    const uint32_t from_page = div_by(from, p.c.page), to_page = div_by(i, p.c.page);
-    const int32_t blk = p.table[static_cast<int64_t>(b) * p.max_blocks + from_page], to = p.dst_table[static_cast<int64_t>(b) * p.dst_max_blocks + to_page];
+    const bool known = static_cast<uint32_t>(from) < static_cast<uint64_t>(p.cap);       // (not if the weights were changed meanwhile)
+    const uint32_t from_page = div_by(known ? from : 0, p.c.page), to_page = div_by(i, p.c.page);
+    const int32_t blk = known ? p.table[static_cast<int64_t>(b) * p.max_blocks + from_page] : -1, to = p.dst_table[static_cast<int64_t>(b) * p.dst_max_blocks + to_page];
     const uint32_t slot = from - from_page * p.c.page.d, to_slot = i - to_page * p.c.page.d;
     if (static_cast<uint32_t>(blk) < static_cast<uint64_t>(p.c.num_blocks) && static_cast<uint32_t>(to) < static_cast<uint64_t>(p.c.num_blocks)) {
       ok = true;

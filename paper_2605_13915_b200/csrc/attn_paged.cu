@@ -913,6 +913,7 @@ struct PagedPlan {
 // (ctas_per_sm: 4, the most of any kernel, where the head dimension is not known; the workspace has room for that)
 bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, PagedPlan* pl) {
   if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 8192 || B > (1 << 20) || Dv < 1 || Dv > 256 || ld < 0 || ld > 0x7FFFFFFF) return false;
+  if (static_cast<int64_t>(B) * Hkv > (1 << 24) || static_cast<double>(B) * (Hq + Hkv) * ld > 1e15) return false;      // (grids and sizes that count)
   const int G = Hq / Hkv;
   pl->slots = G <= 8 ? 8 : kMaxSlots;
   pl->groups = (G + pl->slots - 1) / pl->slots;

@@ -98,6 +98,18 @@ def test_attention_of_many_short_sequences(int8):
     _check_attention(q, c, 0.125, out, lse, before, weights)
 
 
+@pytest.mark.parametrize("D,Dv", [(8, 24), (40, 8), (72, 136), (136, 200)])
+def test_attention_with_odd_head_sizes(D, Dv):
+    """BF16 heads need whole 16 bytes only."""
+    c = make_cache([70, 300], 2, D, Dv, 24, seed=D)
+    q = torch.randn(2, 6, D, generator=torch.Generator().manual_seed(D)).to(torch.bfloat16).cuda()
+    before = torch.zeros(2, 2, 300, device="cuda")
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+
+
 def test_attention_with_more_heads_than_places_on_the_machine():
     """Every CTA walks all sequences of its KV head; one query head each, and 8 groups of 16 for the others."""
     for Hq, Hkv in ((900, 900), (640, 5)):

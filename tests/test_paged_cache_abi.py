@@ -87,6 +87,9 @@ def test_attention_refuses():
     assert need(2, 4, 2, 64) <= need(2, 4, 2, 64, 100) <= need(2, 4, 2, 64, 5000) <= need(64, 4, 2, 64, 5000)
     assert need(64, 32, 8, 128, 8192) >= 64 * 32 * 8192 * 4                       # a score for each head and position
     assert need(2, 5, 2, 64) == 0 and need(2, 4, 2, 512) == 0
+    # sizes that would not fit a launch or an address are refused, not wrapped
+    assert need(1 << 20, 8192, 32, 64) == 0 and need(1 << 20, 8192, 1, 64, (1 << 31) - 1) == 0 and need(1 << 20, 8192, 1, 64, 1 << 31) == 0
+    assert _attend(c, B=1 << 21) == UNSUPPORTED and _attend(c, B=1 << 20, Hq=8192, q_ld=8192 * 64, weights=P, ld=(1 << 31) - 1) == UNSUPPORTED
 
 
 def test_eviction_refuses():

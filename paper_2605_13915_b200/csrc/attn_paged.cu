@@ -950,6 +950,7 @@ msd_status_t launch_paged(const PagedAttnParams& p, cudaStream_t s) {
     cudaGetLastError();
     return MSD_ERR_CUDA;
   }
+  if (p.runs == 1 && !p.weights) return MSD_OK;      // (every sequence was finished by one CTA)
   const unsigned weight_ctas = p.weights ? static_cast<unsigned>(p.B) * p.c.Hkv * p.join_weight_ctas : 0;
   if (launch_pdl(attn_paged_join_kernel, dim3(p.runs * p.U + weight_ctas), dim3(kJoinThreads), p.weights ? p.G * sizeof(float) : 0, s, pdl, p) !=
       cudaSuccess) {

@@ -14,7 +14,7 @@ __device__ __forceinline__ unsigned lanes_below(int lane) { return (1u << lane) 
 // Append.  Bound: HBM for prompts, a chain of latencies for one token a sequence.  A warp takes one new row and some of its KV heads:
 // lanes 0-15 the key, lanes 16-31 the value (16 bytes a lane, twice where D > 128), so the largest element of a row is four
 // shuffles away.  The rows are asked for before the warp looks for the sequence and the page they go to.  14480 rows of 8 heads of 128: BF16
-// 22 us (5.4 TB/s), INT8 28 (3.2 TB/s; without the quantisation 24: the arithmetic issues 60 % of the time); 64 rows INT8 2.8 us.
+// 22 us (5.4 TB/s), INT8 25.3 (3.6 TB/s; the arithmetic issues 60 % of the time); 64 rows INT8 2.6 us.
 // ---------------------------------------------------------------------------------------------------------------------------
 constexpr int kAppendThreads = 128;
 
@@ -46,20 +46,21 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int64_t n, 
   return lo >= 1 && lo <= B ? lo - 1 : -1;
 }
 
-// m / 127 as a true division gives it, by the same corrections as below; what is too small for exact remainders is divided.
+// m / 127 as a true division gives it: an estimate, corrected with its remainder twice, where no remainder underflows (Markstein's
+// theorem: from a neighbour of the quotient and the rounded reciprocal, the correction with an exact remainder is the rounded quotient;
+// P. Markstein, IBM J. Res. Dev. 34, 1990).
 __device__ __forceinline__ float by_127(float m) {
   constexpr float kY = 1.0f / 127.0f;
   float q = m * kY;
   q = __fmaf_rn(__fmaf_rn(-127.0f, q, m), kY, q);
-  q = __fmaf_rn(__fmaf_rn(-127.0f, q, m), kY, q);
-  return m > 1e-28f && m < 1e38f ? q : __fdiv_rn(m, 127.0f);
+  return __fmaf_rn(__fmaf_rn(-127.0f, q, m), kY, q);
 }
 
 // 8 BF16 values -> 8 codes rne(fl(x / s)), two values an instruction and without a branch (rows are full of short integers over a short
-// integer, whose quotients are ties or next to them).  inv is the rounded reciprocal of s; x inv is off by 1.5 units of the quotient's last
-// place at most, one correction with the remainder leaves half a unit and a little, and a second one, from a quotient that is a neighbour of
-// the true one and an exact remainder, is the rounded quotient (P. Markstein, IBM J. Res. Dev. 34, 1990).  Adding 1.5 * 2^23 rounds it half-to-even and leaves
-// the code in the low byte.  (The largest quotient is 127 up to a unit: nothing to clamp.)
+// integer, whose quotients are ties or next to them).  s is fl(m / 127), m the row's largest value, inv about 1 / s.  The estimate x inv,
+// corrected once with its exact remainder, is the quotient up to its last place.  Whether that is enough to round every one as its IEEE quotient rounds
+// depends on the significands of x and m (seven bits each) and the difference of their exponents alone, so the test takes them all.  Adding
+// 1.5 * 2^23 rounds half-to-even and leaves the code in the low byte.  (The largest quotient is 127 up to a unit: nothing to clamp.)
 __device__ __forceinline__ uint2 codes_of(const uint4& v, float s, float inv) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   constexpr float kMagic = 12582912.0f;
@@ -68,17 +69,15 @@ __device__ __forceinline__ uint2 codes_of(const uint4& v, float s, float inv) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint64_t x = pack_f32x2(bf16lo(w[e]), bf16hi(w[e]));
-    uint64_t q = fma_f32x2(x, inv2, zero2);
-    q = fma_f32x2(fma_f32x2(ns2, q, x), inv2, q);
-    q = fma_f32x2(fma_f32x2(ns2, q, x), inv2, q);
-    const float2 r = unpack_f32x2(add_f32x2(q, magic2));
+    const uint64_t q = fma_f32x2(x, inv2, zero2);
+    const float2 r = unpack_f32x2(add_f32x2(fma_f32x2(fma_f32x2(ns2, q, x), inv2, q), magic2));
     c[2 * e] = __float_as_uint(r.x);
     c[2 * e + 1] = __float_as_uint(r.y);
   }
   return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
                     __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
 }
-// The same for a scale that is tiny or huge (or no number), by true divisions.
+// The same for a row whose largest value is tiny or huge (or no number), by true divisions.
 __device__ __noinline__ uint2 codes_by_division(uint4 v, float s) {
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
   unsigned long long out = 0;
@@ -155,9 +154,11 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
           for (int i = 0; i < kVecs; ++i) m = fmaxf(m, unit_absmax(x[a][i]));
 #pragma unroll
           for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-          const float s = by_127(m);
-          const bool plain = s > 1e-30f && s < 1e30f;
-          const float inv = __frcp_rn(s);
+          float s = by_127(m), inv;
+          const bool plain = m > 1e-28f && m < 1e32f;
+          if (!plain) s = __fdiv_rn(m, 127.0f);
+          asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(m));
+          inv *= 127.0f;
 #pragma unroll
           for (int i = 0; i < kVecs; ++i) {
             const int d = (i * 16 + hl) * 8;

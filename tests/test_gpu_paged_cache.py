@@ -120,6 +120,7 @@ def test_attention_with_more_heads_than_places_on_the_machine():
         out, lse = binding.attn_decode_paged(q, *_args(c), 0.25, weights=weights, want_lse=True)
         binding.last_device_status()
         _check_attention(q, c, 0.25, out, lse, before, weights)
+        assert torch.equal(binding.attn_decode_paged(q, *_args(c), 0.25), out)
 
 
 def test_attention_over_a_cache_in_one_piece():
@@ -346,6 +347,29 @@ def test_append_quantises_every_largest_value():
     c = make_cache([n], 1, 16, 16, 64, int8=True, poison=False)
     want = _append_reference(c, rows, rows.flip(2), [0, n])
     binding.kv_append_paged(rows.cuda(), rows.flip(2).contiguous().cuda(), *_args(c), torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    binding.last_device_status()
+    for got, ref in zip((c["k"], c["v"], c["k_scale"].view(torch.int32), c["v_scale"].view(torch.int32)),
+                        (want[0], want[1], want[2].view(torch.int32), want[3].view(torch.int32))):
+        assert torch.equal(got.cpu(), ref)
+
+
+def test_append_quantises_every_pair_of_significands():
+    """Each significand of a row's largest value m with each of x, |x| <= m, at every difference of their exponents that gives a
+    quotient of at least a quarter, both signs: the codes are those of IEEE divisions."""
+    sig = torch.arange(128, 256).float()
+    x = (sig[:, None] * torch.exp2(-torch.arange(10).float())).flatten()          # 1280 values from 255 down to 128 / 512
+    rows = []
+    for m in sig:
+        v = x[x <= m]
+        v = torch.cat([v, -v])
+        v = torch.cat([v, torch.zeros(-len(v) % 127)]).view(-1, 127)
+        rows.append(torch.cat([torch.full((len(v), 1), float(m)), v], 1))
+    rows = torch.cat(rows).to(torch.bfloat16)[:, None]                            # [n, 1, 128], a power of two times small integers: exact
+    n = len(rows)
+    other = (rows.float() * 2.0 ** 60).to(torch.bfloat16)
+    c = make_cache([n], 1, 128, 128, 64, int8=True, poison=False)
+    want = _append_reference(c, rows, other, [0, n])
+    binding.kv_append_paged(rows.cuda(), other.cuda(), *_args(c), torch.tensor([0, n], dtype=torch.int32, device="cuda"))
     binding.last_device_status()
     for got, ref in zip((c["k"], c["v"], c["k_scale"].view(torch.int32), c["v_scale"].view(torch.int32)),
                         (want[0], want[1], want[2].view(torch.int32), want[3].view(torch.int32))):

@@ -625,6 +625,92 @@ def test_decoding_loop(int8):
     binding.last_device_status()
 
 
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_captured_step_decodes_on(int8):
+    """The new token's rows go in and its query attends, in one graph that is replayed with longer sequences each time: every step as
+    the eager calls on a copy of the cache."""
+    Hq, Hkv, D, page, B, width = 8, 2, 128, 16, 3, 5
+    g = torch.Generator().manual_seed(21)
+    c = make_cache([40, 0, 13], Hkv, D, D, page, int8, seed=21, poison=False, spare=B * width)
+    blocks = c["k"].shape[0]
+    tables = torch.randperm(blocks, generator=g)[:B * width].view(B, width).int().cuda()
+    n = torch.zeros(B, dtype=torch.int32, device="cuda")
+    cu = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    kn, vn = (torch.zeros(B, Hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.zeros(B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    pools = [c["k"], c["v"], c["k_scale"], c["v_scale"]]
+    weights, out = torch.zeros(B, Hkv, page * width, device="cuda"), torch.zeros(B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    ws = binding.workspace(binding.attn_decode_paged_workspace_bytes(B, Hq, Hkv, D, page * width))
+
+    def step(pools, n, weights, out):
+        n += 1
+        binding.kv_append_paged(kn, vn, *pools, tables, n, cu, weights=weights)
+        binding.attn_decode_paged(q, *pools, tables, n, 0.1, weights=weights, ws=ws, out=out)
+
+    eager = [None if p is None else p.clone() for p in pools]
+    n2, weights2, out2 = n.clone(), weights.clone(), out.clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step(pools, n, weights, out)
+    n.copy_(torch.tensor([37, 0, 12], dtype=torch.int32))
+    n2.copy_(n)
+    for _ in range(20):
+        for t in (kn, vn, q):
+            t.copy_(torch.randn(t.shape, generator=g))
+        graph.replay()
+        step(eager, n2, weights2, out2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2) and torch.equal(weights, weights2) and torch.equal(n, n2)
+    binding.last_device_status()
+    for a, b in zip(pools, eager):
+        assert a is None or torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """Workspaces of their own, work that overlaps on the GPU: the results are those of the calls alone."""
+    cases = [make_cache([3000, 1200], 4, 128, 128, 16, int8, seed=22 + int8) for int8 in (False, True)]
+    q = torch.randn(2, 16, 128, generator=torch.Generator().manual_seed(22)).to(torch.bfloat16).cuda()
+    want = []
+    for c in cases:
+        w = torch.zeros(2, 4, 3000, device="cuda")
+        want.append((binding.attn_decode_paged(q, *_args(c), 0.1, weights=w), w))
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                w = torch.zeros(2, 4, 3000, device="cuda")
+                got.append((binding.attn_decode_paged(q, *_args(c), 0.1, weights=w), w))
+        torch.cuda.synchronize()
+        for (a, b), (x, y) in zip(want, got):
+            assert torch.equal(a, x) and torch.equal(b, y)
+    binding.last_device_status()
+
+
+def test_append_and_eviction_past_32_bit_offsets():
+    """The last pages of a cache of more than 4 GB."""
+    page, Hkv, D = 64, 8, 128
+    blocks = (5 << 30) // (page * Hkv * D * 2)
+    k = torch.zeros(blocks, page, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    table = torch.arange(blocks - 3, blocks, dtype=torch.int32, device="cuda")[None]
+    dst = torch.tensor([[blocks - 4]], dtype=torch.int32, device="cuda")
+    n, cu = torch.tensor([150], dtype=torch.int32, device="cuda"), torch.tensor([0, 150], dtype=torch.int32, device="cuda")
+    new = torch.randn(2, 150, Hkv, D, generator=torch.Generator().manual_seed(23)).to(torch.bfloat16).cuda()
+    w = torch.zeros(1, Hkv, 150, device="cuda")
+    binding.kv_append_paged(new[0], new[1], k, v, None, None, table, n, cu, weights=w)
+    w[:, :, 60:100] = 1.0
+    _, _, kept = binding.kv_evict_paged(k, v, None, None, table, n, w, 50, dst, recent=7, sinks=3)
+    binding.last_device_status()
+    stay = [0, 1, 2] + list(range(60, 100)) + list(range(143, 150))
+    assert kept[0, 0].tolist() == stay
+    assert torch.equal(k[-3:].flatten(0, 1)[:150], new[0]) and torch.equal(v[-3:].flatten(0, 1)[:150], new[1])
+    assert torch.equal(k[-4, :50], new[0, stay]) and torch.equal(v[-4, :50], new[1, stay])
+    assert not k[:-4].any() and not k[-4, 50:].any()
+
+
 def test_eviction_replays_from_a_graph():
     c, dst = _evict_case([600, 130], 2, 64, 64, 16, 100, True, seed=12)
     w = torch.rand(2, 2, 600, generator=torch.Generator().manual_seed(12)).cuda()

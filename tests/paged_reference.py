@@ -48,6 +48,8 @@ def make_cache(lengths, Hkv, D, Dv, page, int8=False, seed=0, layout="tokens", s
         k, v = laid_out(k), laid_out(v)
     if ks is not None:
         ks, vs = ks.to(device), vs.to(device)
+        if layout == "heads":
+            ks, vs = (x.permute(0, 2, 1).contiguous().permute(0, 2, 1) for x in (ks, vs))
     return {"k": k, "v": v, "k_scale": ks, "v_scale": vs, "table": table.to(device),
             "seqlens": torch.tensor(lengths, dtype=torch.int32, device=device)}
 

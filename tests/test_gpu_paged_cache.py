@@ -240,6 +240,20 @@ def test_attention_gives_equal_bits_and_replays(int8):
     _check_attention(q, c, 0.1, out, None, torch.zeros_like(weights), weights)
 
 
+def test_launches_without_overlap_give_the_same():
+    """Kernels that may start before their predecessors end (and wait for them) against kernels that may not."""
+    c = make_cache([900, 100], 2, 64, 64, 16, int8=True, seed=24)
+    q = torch.randn(2, 8, 64, generator=torch.Generator().manual_seed(24)).to(torch.bfloat16).cuda()
+    got = []
+    for off in (-1, 1):
+        binding.debug_set_option("MSD_NO_PDL", off)
+        w = torch.zeros(2, 2, 900, device="cuda")
+        for _ in range(3):
+            out = binding.attn_decode_paged(q, *_args(c), 0.125, weights=w)
+        got.append((out, w))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
 def test_attention_reports_pages_and_lengths_that_do_not_exist():
     c = make_cache([100, 100], 1, 64, 64, 16, seed=2)
     q = torch.ones(2, 2, 64, dtype=torch.bfloat16, device="cuda")

@@ -707,15 +707,14 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
         for (int w = 0; w < S::kWarps; ++w) {              // (a fixed order)
           const float mw = ml[0][w][h];
-          if (mw != -INFINITY) {
-            const float r = ex2(mw - mh), u = kInt8 ? r * ml[2][w][h] : r;
-            const float4 x = *reinterpret_cast<const float4*>(met + w * (S::kStages * S::kStage / 4) + hl * S::kORow + d);
-            lh = fmaf(ml[1][w][h], r, lh);
-            v.x = fmaf(x.x, u, v.x);
-            v.y = fmaf(x.y, u, v.y);
-            v.z = fmaf(x.z, u, v.z);
-            v.w = fmaf(x.w, u, v.w);
-          }
+          // (a warp without a reference has seen no token, or none whose score is a number: then its sum is none either, and goes on)
+          const float r = mw == -INFINITY ? 0.0f : ex2(mw - mh), u = kInt8 ? r * ml[2][w][h] : r;
+          const float4 x = *reinterpret_cast<const float4*>(met + w * (S::kStages * S::kStage / 4) + hl * S::kORow + d);
+          lh = fmaf(ml[1][w][h], r, lh);
+          v.x = fmaf(x.x, u, v.x);
+          v.y = fmaf(x.y, u, v.y);
+          v.z = fmaf(x.z, u, v.z);
+          v.w = fmaf(x.w, u, v.w);
         }
         if (from_start && to_end) {
           const float inv = 1.0f / lh;
@@ -747,7 +746,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 // (the other CTAs: (sequence, KV head) x share of the positions) from the scores that the first kernel left.
 __device__ __forceinline__ void join_pair(float& m, float& l, float om, float ol) {
   const float mn = fmaxf(m, om);
-  if (mn != -INFINITY) l = l * ex2(m - mn) + ol * ex2(om - mn);
+  l = mn == -INFINITY ? l + ol : l * ex2(m - mn) + ol * ex2(om - mn);      // (no references: no tokens, or no numbers)
   m = mn;
 }
 

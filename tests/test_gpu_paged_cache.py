@@ -173,6 +173,25 @@ def test_attention_with_scores_far_apart(int8):
     _check_attention(q, c, 1.0, out, lse, before, weights)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("length,first,last", [(33, 32, 33), (200, 0, 200), (40000, 0, 2048), (40000, 38016, 40000), (40000, 20000, 20001)])
+def test_attention_passes_nan_on(length, first, last, int8):
+    """Keys that are no numbers, where a warp, a CTA or several of them see nothing else: their KV head's results are none either, and
+    the other head's are what they were."""
+    c = make_cache([length, 50], 2, 64, 64, 16, int8, seed=25)
+    q = torch.randn(2, 8, 64, generator=torch.Generator().manual_seed(25)).to(torch.bfloat16).cuda()
+    weights = [torch.zeros(2, 2, max(length, 50), device="cuda") for _ in range(2)]
+    want, want_lse = binding.attn_decode_paged(q, *_args(c), 0.125, weights=weights[0], want_lse=True)
+    pos = torch.arange(first, last, device="cuda")
+    (c["k_scale"] if int8 else c["k"])[c["table"][0, pos // 16].long(), pos % 16, 1] = float("nan")
+    out, lse = binding.attn_decode_paged(q, *_args(c), 0.125, weights=weights[1], want_lse=True)
+    binding.last_device_status()
+    for got, ref in ((out, want), (lse, want_lse)):
+        assert got[0, 4:].isnan().all() and torch.equal(got[0, :4], ref[0, :4]) and torch.equal(got[1], ref[1])
+    assert weights[1][0, 1, :length].isnan().all() and (weights[1][0, 1, length:] == 0).all() and torch.equal(weights[1][0, 0], weights[0][0, 0])
+    assert torch.equal(weights[1][1], weights[0][1])
+
+
 def test_attention_with_unequal_scales():
     """Values whose scales are a million times apart.  P times the scale is FP16 in units of the largest scale: below 2^-21 of it the
     error is 2^-32 of that scale (rounded up to a power of two) for each token, times its code."""

@@ -734,7 +734,8 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     }
     if (threadIdx.x == 0) {                      // the runs that have tiles of this sequence
       const int64_t at = static_cast<int64_t>(end) - cur.left - seg - seg_first, upto = at + (L + S::kTile - 1) / S::kTile;
-      const int run0 = static_cast<int>(((at + 1) * runs - 1) / T), run1 = static_cast<int>((upto * runs - 1) / T);
+      // (between 0 and runs - 1, and apart where the sequence is cut, unless the lengths are changed meanwhile)
+      const int run0 = max(static_cast<int>(((at + 1) * runs - 1) / T), 0), run1 = min(static_cast<int>((upto * runs - 1) / T), runs - 1);
       if (from_start && unit == 0) p.seq_runs[b] = make_int2(run0, run1);
       if (!to_end) p.tail[blockIdx.x] = make_int4(b, run0, run1, 0);
     }
@@ -769,6 +770,7 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
     // sixteen, 7.9 with four).
     const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
     const int n = tail.z - tail.y + 1, helpers = n - 1, helper = run - tail.y;
+    if (n < 2) return;
     const int Dv = p.c.Dv, vecs = Dv / 4, all = nh * vecs;
     const int item0 = all * helper / helpers, items = all * (helper + 1) / helpers - item0;
     if (items == 0) return;
@@ -841,7 +843,8 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
 
   const int w = blockIdx.x - join_ctas, share = w % p.join_weight_ctas, bk = w / p.join_weight_ctas;
   const int b = bk / p.c.Hkv, hk = bk - b * p.c.Hkv;
-  const int2 span = p.seq_runs[b];               // (anything at all for an empty sequence)
+  int2 span = p.seq_runs[b];                     // (anything at all for an empty sequence, and for one that has just stopped being one)
+  span = make_int2(max(span.x, 0), min(span.y, p.runs - 1));
   const int L = seq_len(p, b);
   if (L == 0 || static_cast<int64_t>(share) * kJoinThreads >= L) return;
   for (int g = tid >> 5; g < p.G; g += kJoinThreads / 32) {
@@ -1018,6 +1021,13 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   if (!rows_within(p.c.k, blocks, page, most_rows) || !rows_within(p.c.v, blocks, page, most_rows) ||
       (int8 && !(rows_within(p.c.ks, blocks, page, most_scales) && rows_within(p.c.vs, blocks, page, most_scales))))
     return MSD_ERR_UNSUPPORTED;
+  // (positions stay below 2^31 - the tokens of a tile, and tiles below 2^31, so that no sum of theirs wraps)
+  p.cap = static_cast<int64_t>(max_blocks) * cache->page_size;
+  if (weights && p.cap > ld) p.cap = ld;
+  if (p.cap > 0x7FFFF000) p.cap = 0x7FFFF000;
+  const int tile = with_shape(int8, widest, slots, TileTokens{});
+  const int64_t room = (p.cap + tile - 1) / tile * B;
+  if (room > 0x7FFFFFFF) return MSD_ERR_UNSUPPORTED;
   p.k_block = static_cast<uint32_t>(p.c.k.block / 16);
   p.k_token = static_cast<uint32_t>(p.c.k.token / 16);
   p.v_block = static_cast<uint32_t>(p.c.v.block / 16);
@@ -1034,10 +1044,6 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.table = block_table;
   p.seqlens = seqlens;
   p.max_blocks = max_blocks;
-  // (positions stay below 2^31 - the tokens of a tile, so that no sum of theirs wraps)
-  p.cap = static_cast<int64_t>(max_blocks) * cache->page_size;
-  if (weights && p.cap > ld) p.cap = ld;
-  if (p.cap > 0x7FFFF000) p.cap = 0x7FFFF000;
   // Keys and values that L2 can hold a part of until the next step leave it before anything else does, or a part of them is never there
   // when it is asked for again: 64/8 heads, 24 x 512-4096 tokens INT8 34.3 / 32.4 us without / with, 16/16 heads of 80, 48 x 0-1500 51 / 47;
   // of more than that nothing stays either way, and it costs 3 % (2 x 100000-131072 BF16 164 / 169 us).
@@ -1048,8 +1054,6 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.groups = pl.groups;
   p.U = pl.U;
   // no more runs than tiles that the sequences have room for (their lengths are on the device)
-  const int tile = with_shape(int8, widest, slots, TileTokens{});
-  const int64_t room = (p.cap + tile - 1) / tile * B;
   p.runs = room < pl.runs ? static_cast<int>(room) : pl.runs;
   p.scale2 = softmax_scale * 1.4426950408889634f;
   p.out = static_cast<uint16_t*>(out_bf16);

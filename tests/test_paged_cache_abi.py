@@ -90,6 +90,7 @@ def test_attention_refuses():
     # sizes that would not fit a launch or an address are refused, not wrapped
     assert need(1 << 20, 8192, 32, 64) == 0 and need(1 << 20, 8192, 1, 64, (1 << 31) - 1) == 0 and need(1 << 20, 8192, 1, 64, 1 << 31) == 0
     assert _attend(c, B=1 << 21) == UNSUPPORTED and _attend(c, B=1 << 20, Hq=8192, q_ld=8192 * 64, weights=P, ld=(1 << 31) - 1) == UNSUPPORTED
+    assert _attend(c, B=1 << 16, max_blocks=1 << 27, room=1 << 40) == UNSUPPORTED and _attend(c, B=1 << 16, max_blocks=1 << 27, room=0) == ROOM
 
 
 def test_eviction_refuses():

@@ -136,39 +136,48 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 
-// DP: D and Dv rounded up to 64, 128 or 256; kHeads: head slots of a CTA, 8 or 16.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB of
-// keys and values; the rings of all CTAs of an SM together hold about 200 KB, and more warps with two stages were better than fewer
-// with three (heads of 128, 32 x 2048-8192 tokens: INT8 81 / 85 us, 16 / 16 heads of 80 52 / 57; heads of 64 BF16 60 / 63).
+// DP: D and Dv rounded up to 64, 96, 128, 192 or 256; kHeads: head slots of a CTA, 8 or 16.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB
+// of keys and values; the rings of an SM's CTAs hold 140 to 200 KB.  Two stages and as many warps as their registers allow (heads of 128, 32 x
+// 2048-8192 tokens: INT8 81 / 85 us, 16 / 16 heads of 80 52 / 57 with more stages and fewer warps; at the same number of warps a third
+// stage, 24 x 1024-4096: 16 / 16 heads of 64 INT8 39.9 / 44.0, of 256 99 / 101), but for BF16 with two CTAs an SM (128 / 8 heads of 128: 53.5 with two
+// stages, 52.6 with three).  Sizes of 96 and 192 beside the powers of two: 128 / 8 heads of 80 BF16 48 -> 42 us, INT8 45 -> 39, 16 / 16 heads
+// of 96 INT8 57 -> 50, of 192 BF16 128 -> 122, INT8 92 -> 78.
 template <bool kInt8, int DP, int kHeads>
 struct Shape {
   static constexpr int kWarps = !kInt8 && DP == 256 ? 6 : 4;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kEs = kInt8 ? 1 : 2;
-  static constexpr int kTok = DP == 64 || (kInt8 && DP == 128) ? 32 : 16;
+  static constexpr int kTok = DP == 64 || (kInt8 && DP <= (kHeads == 8 ? 128 : 192)) ? 32 : 16;
   static constexpr int kRow = DP * kEs;                         // bytes of a row in shared memory
   static constexpr int kHalf = kTok * kRow;                     // keys, then values
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
-  static constexpr bool kWide = kHalf >= 4096;                  // 8 KB a tile and more
-  static constexpr int kCtasPerSm = kHalf >= 8192 ? 1 : (kWide ? (DP <= 128 && kHeads == 8 ? 3 : 2) : (kHeads == 8 ? 4 : 3));
-  static constexpr int kStages = kWide ? (kCtasPerSm == 3 || kHalf >= 8192 ? 2 : 3) : (kHeads == 8 ? 3 : 4);
+  static constexpr int kCtasPerSm = !kInt8 && DP == 256  ? 1
+                                    : kInt8 && DP == 64  ? (kHeads == 8 ? 4 : 3)
+                                    : DP == 96 || (kHeads == 8 && DP <= (kInt8 ? 192 : 128)) ? 3
+                                                         : 2;
   static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
+  static constexpr int kQBytes = kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0, kStatic = 2304;
+  static constexpr int kStages = !kInt8 && kCtasPerSm == 2 && 2 * kWarps * 3 * kStage <= 200 * 1024 ? 3 : 2;
   static constexpr int kRing = kWarps * kStages * kStage;
   // The warps' outputs meet in the stages that their last tiles left, all heads or 8 at a time; rows four words apart in the banks
   // where there is room for that.
   static constexpr int kMeet = kHeads * DP * 4 <= kStage ? kHeads : 8;
   static constexpr int kORow = kMeet * (DP + 4) * 4 <= kStage ? DP + 4 : DP;
-  static constexpr int kSmem = kRing + (kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0);
+  static constexpr int kSmem = kRing + kQBytes;
   static constexpr int kTile = kWarps * kTok;                  // tokens of a CTA's tile
   static_assert(kMeet * kORow * 4 <= kStage, "a stage has to hold a warp's outputs");
-  static_assert(kCtasPerSm * (kSmem + 2304) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
+  static_assert(kCtasPerSm * (kSmem + kStatic) <= 228 * 1024, "the CTAs of an SM have to fit its shared memory");
 };
 
-// 16-byte chunk c of row r, so that the eight rows of a matrix lie in different banks
+// 16-byte chunk c of row r, so that the eight rows of a matrix lie in different banks: as many bits of the row as its length leaves alike
+// are exclusive-ored into the chunk's number (rows of 8, 4 or 2 chunks times an odd number start at 1, 2 or 4 places in the banks).
 template <int kRow>
-__device__ __forceinline__ uint32_t swz(int r, int c) {
-  return r * kRow + ((c ^ (kRow >= 128 ? (r & 7) : ((r >> 1) & 3))) << 4);
-}
+struct Swizzle {
+  static constexpr int kMask = kRow % 128 == 0 ? 7 : (kRow % 64 == 0 ? 3 : 1), kShift = kMask == 7 ? 0 : (kMask == 3 ? 1 : 2);
+  static __device__ __forceinline__ uint32_t bits(int r) { return (r >> kShift) & kMask; }
+  static __device__ __forceinline__ uint32_t at(int r, int c) { return r * kRow + ((c ^ bits(r)) << 4); }
+};
 
 __device__ __forceinline__ int seq_len(const PagedAttnParams& p, int b) {
   const int32_t n = p.seqlens[b];
@@ -259,9 +268,12 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   const uint64_t policy = p.leave_l2 ? policy_evict_first() : policy_evict_normal();
   uint8_t* ring = smem + warp * (S::kStages * S::kStage);
   const uint32_t ring_u = smem_u32(ring);
+  using W = Swizzle<S::kRow>;
   constexpr int kChunks = S::kRow / 16;                 // 16-byte chunks of a row
-  constexpr int kRowsPer = 32 / kChunks;                // rows that one instruction of the warp brings
-  const int my_chunk = lane % kChunks, my_row = lane / kChunks;
+  constexpr int kLanes = kChunks <= 4 ? 4 : (kChunks <= 8 ? 8 : (kChunks <= 16 ? 16 : 32));      // lanes that bring a row, some of them idle
+  constexpr int kRowsPer = 32 / kLanes;                 // rows that one instruction of the warp brings
+  const int my_chunk = lane % kLanes, my_row = lane / kLanes;
+  const bool busy = kLanes == kChunks || my_chunk < kChunks;
   const uint8_t* kbase = p.c.k.base + hk * p.c.k.head + my_chunk * 16;
   const uint8_t* vbase = p.c.v.base + hk * p.c.v.head + my_chunk * 16;
   const uint8_t* ksbase = kInt8 ? p.c.ks.base + hk * p.c.ks.head : nullptr;
@@ -271,7 +283,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   // the others get its offset by a shuffle whose index is a constant.
   constexpr int kIter = S::kTok / kRowsPer;
   const int tok_lane = my_chunk % kIter * kRowsPer + my_row;
-  const uint32_t lane_dst = S::kRow >= 128 ? my_row * S::kRow + ((my_chunk ^ my_row) << 4) : swz<S::kRow>(my_row, my_chunk);
+  const uint32_t lane_dst = W::at(my_row, my_chunk);
   // The block of this lane's token of the tile that `ld` stands on, asked for a tile ahead; -1 behind the end.
   const int32_t* ld_table = p.table + static_cast<int64_t>(ld.b) * p.max_blocks;
   int ld_pos = ld.tile * S::kTile + warp * S::kTok + tok_lane;
@@ -295,20 +307,31 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       const uint32_t ko = at * p.k_block + in * p.k_token, vo = at * p.v_block + in * p.v_token;
       const uint32_t mask = __ballot_sync(0xffffffffu, there);
       const uint32_t at_k = dst + lane_dst, at_v = at_k + S::kHalf;
-      auto to = [&](uint32_t base, int i) { return (base ^ (S::kRow >= 128 ? ((i * kRowsPer) & 7) << 4 : 0)) + i * kRowsPer * S::kRow; };
-      if (__all_sync(0xffffffffu, mask == 0xffffffffu && k_there && v_there)) {
+      auto to = [&](uint32_t base, int i) { return (base ^ (W::bits(i * kRowsPer) << 4)) + i * kRowsPer * S::kRow; };
+      auto from = [&](const uint8_t* base, uint32_t off, int i) { return base + static_cast<uint64_t>(__shfl_sync(0xffffffffu, off, i, kLanes)) * 16; };
+      if (__all_sync(0xffffffffu, mask == 0xffffffffu && ((k_there && v_there) || !busy))) {
 #pragma unroll
-        for (int i = 0; i < kIter; ++i) cp16_all(to(at_k, i), kbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, ko, i, kChunks)) * 16, policy);
+        for (int i = 0; i < kIter; ++i) {
+          const uint8_t* src = from(kbase, ko, i);
+          if (busy) cp16_all(to(at_k, i), src, policy);
+        }
 #pragma unroll
-        for (int i = 0; i < kIter; ++i) cp16_all(to(at_v, i), vbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, vo, i, kChunks)) * 16, policy);
+        for (int i = 0; i < kIter; ++i) {
+          const uint8_t* src = from(vbase, vo, i);
+          if (busy) cp16_all(to(at_v, i), src, policy);
+        }
       } else {                                          // zeros for rows behind the end and for values that a row does not have
-        const uint32_t mine = mask >> (my_row * kChunks), k_mask = k_there ? mine : 0u, v_mask = v_there ? mine : 0u;
+        const uint32_t mine = mask >> (my_row * kLanes), k_mask = k_there ? mine : 0u, v_mask = v_there ? mine : 0u;
 #pragma unroll
-        for (int i = 0; i < kIter; ++i)
-          cp16(to(at_k, i), kbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, ko, i, kChunks)) * 16, (k_mask >> i) & 1u, policy);
+        for (int i = 0; i < kIter; ++i) {
+          const uint8_t* src = from(kbase, ko, i);
+          if (busy) cp16(to(at_k, i), src, (k_mask >> i) & 1u, policy);
+        }
 #pragma unroll
-        for (int i = 0; i < kIter; ++i)
-          cp16(to(at_v, i), vbase + static_cast<uint64_t>(__shfl_sync(0xffffffffu, vo, i, kChunks)) * 16, (v_mask >> i) & 1u, policy);
+        for (int i = 0; i < kIter; ++i) {
+          const uint8_t* src = from(vbase, vo, i);
+          if (busy) cp16(to(at_v, i), src, (v_mask >> i) & 1u, policy);
+        }
       }
       if constexpr (kInt8) {
         const uint32_t sc = dst + 2 * S::kHalf + tok_lane * 4;
@@ -419,11 +442,11 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   for (int n = 0; n < NT; ++n) f[n][0] = f[n][1] = p.scale2;
 
   // Matrices of the fragments: token (lane & 15) of 16, chunks c and c + 1 by the upper half of the warp; BF16 values: tokens by the upper
-  // half, chunks by the eighths.  The swizzle moves only the lowest three bits of a chunk's number (two where a row is 64 bytes), so
+  // half, chunks by the eighths.  The swizzle moves only the lowest bits of a chunk's number, so
   // chunk c is an exclusive or away from chunk 0, and what lies above those bits an offset.
-  const uint32_t k_lane = swz<S::kRow>(lane & 15, lane >> 4);
-  const uint32_t v_lane = S::kHalf + (kInt8 ? k_lane : swz<S::kRow>(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
-  constexpr int kSwz = S::kRow >= 128 ? 7 : 3;
+  const uint32_t k_lane = W::at(lane & 15, lane >> 4);
+  const uint32_t v_lane = S::kHalf + (kInt8 ? k_lane : W::at(((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
+  constexpr int kSwz = W::kMask;
   uint32_t stage_u = ring_u, fill_u = ring_u + (S::kStages - 1) * S::kStage;      // the stage of this tile, and the one to fill
   const float* stage_scales = reinterpret_cast<const float*>(ring + 2 * S::kHalf);
   fetch_q();
@@ -472,7 +495,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         for (int c4 = 0; c4 < kSteps; c4 += 4) {        // 64 values of d at a time: what is past D is zero in both
           if (c4 >= k_steps) break;
 #pragma unroll
-          for (int c = c4; c < c4 + 4; c += kInt8 ? 2 : 1) {
+          for (int c = c4; c < c4 + 4 && c < kSteps; c += kInt8 ? 2 : 1) {
             uint32_t r[4];
             const int chunk = kInt8 ? c : 2 * c;
             ldsm4(r, (k_u ^ ((chunk & kSwz) << 4)) + ((chunk & ~kSwz) << 4) + g * 16 * S::kRow);
@@ -626,7 +649,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         for (int c4 = 0; c4 < DP / 16; c4 += 4) {
           if (c4 >= v_steps) break;
 #pragma unroll
-          for (int c = c4; c < c4 + 4; c += kInt8 ? 2 : 1) {
+          for (int c = c4; c < c4 + 4 && c < kSteps; c += kInt8 ? 2 : 1) {
             uint32_t r[4];
             const int chunk = kInt8 ? c : 2 * c;
             ldsm4_t(r, (v_u ^ ((chunk & kSwz) << 4)) + ((chunk & ~kSwz) << 4) + g * 16 * S::kRow);
@@ -971,8 +994,11 @@ auto with_shape(bool int8, int widest, int slots, F&& f) {
     return slots == 8 ? f.template operator()<decltype(i8)::value, decltype(dp)::value, 8>() : f.template operator()<decltype(i8)::value, decltype(dp)::value, 16>();
   };
   auto size = [&](auto i8) {
-    return widest <= 64 ? heads(i8, std::integral_constant<int, 64>{})
-                        : (widest <= 128 ? heads(i8, std::integral_constant<int, 128>{}) : heads(i8, std::integral_constant<int, 256>{}));
+    if (widest <= 64) return heads(i8, std::integral_constant<int, 64>{});
+    if (widest <= 96) return heads(i8, std::integral_constant<int, 96>{});
+    if (widest <= 128) return heads(i8, std::integral_constant<int, 128>{});
+    if (widest <= 192) return heads(i8, std::integral_constant<int, 192>{});
+    return heads(i8, std::integral_constant<int, 256>{});
   };
   return int8 ? size(std::true_type{}) : size(std::false_type{});
 }

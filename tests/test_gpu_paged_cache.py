@@ -110,6 +110,20 @@ def test_attention_with_odd_head_sizes(D, Dv):
     _check_attention(q, c, D ** -0.5, out, lse, before, weights)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("G", [2, 11])
+@pytest.mark.parametrize("D,Dv", [(80, 96), (96, 80), (160, 64), (128, 192), (192, 144), (208, 256)])
+def test_attention_with_every_width_of_a_row(D, Dv, G, int8):
+    """Rows are laid out in shared memory by the wider of a key and a value, rounded up to 64, 96, 128, 192 or 256."""
+    c = make_cache([333, 0, 64, 700, 17], 2, D, Dv, 16, int8, seed=D + G, layout="heads")
+    q = torch.randn(5, 2 * G, D, generator=torch.Generator().manual_seed(D)).to(torch.bfloat16).cuda()
+    before = torch.rand(5, 2, 700, generator=torch.Generator().manual_seed(G)).cuda()
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+
+
 def test_attention_with_more_heads_than_places_on_the_machine():
     """Every CTA walks all sequences of its KV head; one query head each, and 8 groups of 16 for the others."""
     for Hq, Hkv in ((900, 900), (640, 5)):

@@ -44,6 +44,8 @@ namespace {
 
 constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
+constexpr int kAtOnceWeights = 4;           // positions of a thread whose scores are under way together
+constexpr int kClusterTiles = 4, kClusterCtas = 16;
 constexpr float kHeld = 8.0f;               // how far (log2) a score may exceed its reference before that moves
 constexpr float kPUnits = 128.0f;           // INT8: 2^15 / 2^kHeld
 
@@ -184,7 +186,185 @@ __device__ __forceinline__ int seq_len(const PagedAttnParams& p, int b) {
   return static_cast<int>(min(static_cast<int64_t>(n < 0 ? 0 : n), p.cap));
 }
 
-template <bool kInt8, int DP, int kHeads>
+// ---- what is left when all CTAs of a unit are done: cut sequences are joined, scores become weights ----
+
+template <int kThreads>      // among the kThreads threads that use this barrier
+__device__ __forceinline__ void sync_threads(int barrier) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(kThreads) : "memory"); }
+
+__device__ __forceinline__ void join_pair(float& m, float& l, float om, float ol) {
+  const float mn = fmaxf(m, om);
+  l = mn == -INFINITY ? l + ol : l * ex2(m - mn) + ol * ex2(om - mn);      // (no references: no tokens, or no numbers)
+  m = mn;
+}
+
+// This CTA's part of joining the sequence that is cut at the end of its run (tail: sequence or -1, its first and last run).  The CTAs of
+// all runs but the last one that have tiles of the sequence share the join: each takes some of the outputs, four values of a head an item, and
+// some threads an item, which take some of the pieces (slot 1 of the first run, slot 0 of the others).  At most four threads an item: more
+// shorten the walk over the pieces by less than the exchange at its end takes (B = 1, 1001 tokens, in two kernels: 8.3 us with sixteen, 7.9 with
+// four).
+template <int kThreads>
+__device__ __forceinline__ void join_tail(const PagedAttnParams& p, int tid, int barrier, int unit, int run, const int4& tail, float4* sums, float2* mls) {
+  if (tail.x < 0) return;
+  const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
+  const int n = tail.z - tail.y + 1, helpers = n - 1, helper = run - tail.y;
+  if (n < 2) return;
+  const int Dv = p.c.Dv, vecs = Dv / 4, all = nh * vecs;
+  const int item0 = all * helper / helpers, items = all * (helper + 1) / helpers - item0;
+  if (items == 0) return;
+  const int share = items >= kThreads ? 1 : min(min(kThreads / items, 4), n), at_once = kThreads / share;
+  const int my = tid / share, part = tid - my * share;
+  const int64_t out0 = static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0;
+  for (int base = 0; base < items; base += at_once) {
+    const bool on = my < at_once && base + my < items;
+    const int item = item0 + base + my, r = item / vecs, d = (item - r * vecs) * 4;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float m = -INFINITY, l = 0.0f;
+    if (on) {                                  // maximum, sum and output together: one round trip to memory for four pieces
+      constexpr int kPieces = 4;
+      for (int i0 = part; i0 < n; i0 += share * kPieces) {
+        float2 ml[kPieces];
+        float4 x[kPieces];
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          const int i = i0 + k * share;
+          if (i < n) {
+            const int64_t s = ((static_cast<int64_t>(tail.y + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + r;
+            ml[k] = *reinterpret_cast<const float2*>(p.part_ml + s * 2);
+            x[k] = *reinterpret_cast<const float4*>(p.part + s * Dv + d);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          if (i0 + k * share < n) {
+            const float mn = fmaxf(m, ml[k].x);
+            const float a = m == -INFINITY ? 0.0f : ex2(m - mn), w = ml[k].x == -INFINITY ? 0.0f : ex2(ml[k].x - mn);
+            m = mn;
+            l = l * a + ml[k].y * w;
+            acc.x = acc.x * a + x[k].x * w;
+            acc.y = acc.y * a + x[k].y * w;
+            acc.z = acc.z * a + x[k].z * w;
+            acc.w = acc.w * a + x[k].w * w;
+          }
+        }
+      }
+    }
+    if (share > 1) {
+      sync_threads<kThreads>(barrier);
+      sums[tid] = acc;
+      mls[tid] = make_float2(m, l);
+      sync_threads<kThreads>(barrier);
+    }
+    if (on && part == 0) {
+      if (share > 1) {
+        for (int i = 1; i < share; ++i) m = fmaxf(m, mls[tid + i].x);
+        l = 0.0f;
+        acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < share; ++i) {
+          const float2 ml = mls[tid + i];
+          const float w = ml.x == -INFINITY ? 0.0f : ex2(ml.x - m);
+          const float4 x = sums[tid + i];
+          l = fmaf(ml.y, w, l);
+          acc.x = fmaf(x.x, w, acc.x);
+          acc.y = fmaf(x.y, w, acc.y);
+          acc.z = fmaf(x.z, w, acc.z);
+          acc.w = fmaf(x.w, w, acc.w);
+        }
+      }
+      const float inv = 1.0f / l;
+      *reinterpret_cast<uint2*>(p.out + (out0 + r) * Dv + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      if (d == 0 && p.lse) p.lse[out0 + r] = (m + log2f(l)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// Adds the weights of positions first + tid, first + tid + step ... below `end` of sequence b; span: the first and the last run that have tiles
+// of it.  A block of threads, or a warp where no KV head has more than 8 query heads.  The first scores are asked for before the sums of the
+// softmax that they wait for.
+template <int kThreads>
+__device__ __forceinline__ void add_weights(const PagedAttnParams& p, int tid, int b, int hk, int2 span, int first, int step, int end, float* lse2_sm) {
+  constexpr int kAtOnce = kAtOnceWeights;
+  const int64_t at = (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + first + tid, score_step = static_cast<int64_t>(step) * p.score_heads;
+  const float* s = p.scores + at * p.score_heads;
+  float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld + first + tid;
+  const bool four = p.score_heads == 4;          // the ordinary number: one load a position
+  int left = end - first - tid;
+  float4 x[kAtOnce];
+  float was[kAtOnce];
+  auto fetch = [&]() {
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (left <= i * step) break;
+      was[i] = out[static_cast<int64_t>(i) * step];
+      if (four) {
+        x[i] = __ldcg(reinterpret_cast<const float4*>(s + i * score_step));
+      } else {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(s + i * score_step));
+        x[i] = make_float4(y.x, y.y, 0.0f, 0.0f);
+      }
+    }
+  };
+  fetch();
+  // log2 of the sum of 2^score of head g, from pieces lane, lane + lanes, ...
+  auto lse2 = [&](int g, int lane, int lanes) {
+    if (span.x == span.y) return p.lse2[static_cast<int64_t>(b) * p.Hq + hk * p.G + g];
+    const int unit = hk * p.groups + g / p.slots, r = g % p.slots;
+    float m = -INFINITY, l = 0.0f;
+    for (int i = lane; i <= span.y - span.x; i += lanes) {
+      const int64_t slot = (static_cast<int64_t>(span.x + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0);
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (slot * p.part_rows + r) * 2);
+      join_pair(m, l, ml.x, ml.y);
+    }
+    for (int d = lanes / 2; d > 0; d >>= 1) {
+      const float om = __shfl_xor_sync(0xffffffffu, m, d), ol = __shfl_xor_sync(0xffffffffu, l, d);
+      join_pair(m, l, om, ol);
+    }
+    return m + log2f(l);
+  };
+  if constexpr (kThreads == 32) {                // four lanes a head
+    const float lg = lse2(min(tid >> 2, p.G - 1), tid & 3, 4);
+    __syncwarp();
+    if ((tid & 3) == 0) lse2_sm[tid >> 2] = lg;
+    __syncwarp();
+  } else {
+    for (int g = tid >> 5; g < p.G; g += kThreads / 32) {
+      const float lg = lse2(g, tid & 31, 32);
+      if ((tid & 31) == 0) lse2_sm[g] = lg;
+    }
+    __syncthreads();
+  }
+  // (no weight for a head that is not there)
+  const float l0 = lse2_sm[0], l1 = p.G > 1 ? lse2_sm[1] : INFINITY, l2 = four ? lse2_sm[2] : INFINITY, l3 = four && p.G > 3 ? lse2_sm[3] : INFINITY;
+  while (left > 0) {
+    float acc[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      acc[i] = ex2(x[i].x - l0) + (l1 != INFINITY ? ex2(x[i].y - l1) : 0.0f);
+      if (four) acc[i] = acc[i] + ex2(x[i].z - l2) + (l3 != INFINITY ? ex2(x[i].w - l3) : 0.0f);
+    }
+    if (!four) {
+      for (int g = 2; g < p.G; g += 2) {
+        const float la = lse2_sm[g], lb = g + 1 < p.G ? lse2_sm[g + 1] : INFINITY;
+        float2 y[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (left > i * step) y[i] = __ldcg(reinterpret_cast<const float2*>(s + i * score_step + g));
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (left > i * step) acc[i] += ex2(y[i].x - la) + (lb != INFINITY ? ex2(y[i].y - lb) : 0.0f);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if (left > i * step) out[static_cast<int64_t>(i) * step] = was[i] + acc[i];
+    left -= step * kAtOnce;
+    s += score_step * kAtOnce;
+    out += static_cast<int64_t>(step) * kAtOnce;
+    fetch();
+  }
+}
+
+// kJoin: the CTAs of a unit are a cluster, which joins its sequences and adds their weights itself.
+template <bool kInt8, int DP, int kHeads, bool kJoin>
 __global__ void __launch_bounds__((Shape<kInt8, DP, kHeads>::kThreads), (Shape<kInt8, DP, kHeads>::kCtasPerSm))
 attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   using S = Shape<kInt8, DP, kHeads>;
@@ -192,7 +372,8 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ float ml[3][S::kWarps][kHeads];              // of a warp: references, sums, units of its outputs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
+  __shared__ int4 tail_sm;                               // (kJoin)
+  const int unit = kJoin ? blockIdx.x / p.runs : blockIdx.x % p.U, run = kJoin ? blockIdx.x % p.runs : blockIdx.x / p.U;
   const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kHeads;        // first head of the group within the KV head
   const int nh = min(p.G - h0, kHeads);
   const int64_t head0 = static_cast<int64_t>(hk) * p.G + h0;
@@ -226,9 +407,38 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   }
   const int T = __shfl_sync(0xffffffffu, before, 31);
   before -= mine;
-  if (threadIdx.x == 0) p.tail[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  int4* tail = kJoin ? &tail_sm : p.tail + blockIdx.x;
+  if (threadIdx.x == 0) *tail = make_int4(-1, 0, 0, 0);
   const int runs = min(p.runs, T);                // (no empty runs)
-  if (run >= runs) return;
+  auto meet_cluster = [&]() {                     // every CTA of the unit is done; the rings are free
+    cluster_arrive_all();
+    cluster_wait_all();
+    float4* sums = reinterpret_cast<float4*>(smem);
+    float2* mls = reinterpret_cast<float2*>(sums + S::kThreads);
+    float* lse2_sm = reinterpret_cast<float*>(mls + S::kThreads);
+    constexpr int kHalf = S::kThreads / 2;        // half of the warps join while the others add weights
+    if (threadIdx.x < kHalf) join_tail<kHalf>(p, threadIdx.x, 1, unit, run, tail_sm, sums, mls);
+    if (threadIdx.x < kHalf || !p.weights) return;
+    // (blocks of positions, dealt out to the warps of all CTAs sequence after sequence)
+    constexpr int kBlock = 32 * kAtOnceWeights, kAdders = S::kWarps - S::kWarps / 2;
+    const int adders = p.runs * kAdders, adder = run * kAdders + warp - S::kWarps / 2;
+    lse2_sm += warp * 8;
+    int64_t at = 0;
+    int turn = 0;
+    for (int b = 0; b < p.B && T > 0; ++b) {
+      const int L = seq_len(p, b), blocks = (L + kBlock - 1) / kBlock;
+      const int64_t upto = at + (L + S::kTile - 1) / S::kTile;
+      const int run0 = static_cast<int>(((at + 1) * runs - 1) / T), run1 = min(static_cast<int>((upto * runs - 1) / T), runs - 1);
+      for (int i = adder >= turn ? adder - turn : adder - turn + adders; i < blocks; i += adders)
+        add_weights<32>(p, lane, b, hk, make_int2(run0, run1), i * kBlock, 32, min(L, (i + 1) * kBlock), lse2_sm);
+      at = upto;
+      turn = (turn + blocks) % adders;
+    }
+  };
+  if (run >= runs) {
+    if constexpr (kJoin) meet_cluster();
+    return;
+  }
   auto run_start = [&](int r) { return static_cast<int>(static_cast<int64_t>(r) * T / runs); };
   const int first = run_start(run), end = run_start(run + 1);
   const bool here = first >= before && first < before + mine;       // of one lane
@@ -695,7 +905,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     }
     const bool from_start = seg_first == 0, to_end = seg_first + seg == (L + S::kTile - 1) / S::kTile;
     const int Dv = p.c.Dv, vecs = Dv / 4;
-    const int64_t slot = static_cast<int64_t>(blockIdx.x) * 2 + (from_start ? 1 : 0);
+    const int64_t slot = (kJoin ? static_cast<int64_t>(run) * p.U + unit : static_cast<int64_t>(blockIdx.x)) * 2 + (from_start ? 1 : 0);
     float* meet = reinterpret_cast<float*>(smem + (fill_u - smem_u32(smem)));      // this warp's stage; the others' are as far from their rings
 #pragma unroll
     for (int pass = 0; pass < kHeads / S::kMeet; ++pass) {
@@ -759,21 +969,16 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
       const int64_t at = static_cast<int64_t>(end) - cur.left - seg - seg_first, upto = at + (L + S::kTile - 1) / S::kTile;
       // (between 0 and runs - 1, and apart where the sequence is cut, unless the lengths are changed meanwhile)
       const int run0 = max(static_cast<int>(((at + 1) * runs - 1) / T), 0), run1 = min(static_cast<int>((upto * runs - 1) / T), runs - 1);
-      if (from_start && unit == 0) p.seq_runs[b] = make_int2(run0, run1);
-      if (!to_end) p.tail[blockIdx.x] = make_int4(b, run0, run1, 0);
+      if (!kJoin && from_start && unit == 0) p.seq_runs[b] = make_int2(run0, run1);
+      if (!to_end) *tail = make_int4(b, run0, run1, 0);
     }
   }
   cp_wait<0>();
+  if constexpr (kJoin) meet_cluster();
 }
 
 // Joins the partial results of cut sequences (CTAs [0, runs x U), those whose run ends inside one), and adds the attention weights
 // (the other CTAs: (sequence, KV head) x share of the positions) from the scores that the first kernel left.
-__device__ __forceinline__ void join_pair(float& m, float& l, float om, float ol) {
-  const float mn = fmaxf(m, om);
-  l = mn == -INFINITY ? l + ol : l * ex2(m - mn) + ol * ex2(om - mn);      // (no references: no tokens, or no numbers)
-  m = mn;
-}
-
 __global__ void __launch_bounds__(kJoinThreads)
 attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
   __shared__ float4 sums[kJoinThreads];
@@ -782,154 +987,17 @@ attn_paged_join_kernel(const __grid_constant__ PagedAttnParams p) {
   pdl_wait_primary();
   pdl_launch_dependents();
   const int join_ctas = p.runs * p.U;
-  const int tid = threadIdx.x;
   if (static_cast<int>(blockIdx.x) < join_ctas) {
-    const int unit = blockIdx.x % p.U, run = blockIdx.x / p.U;
-    const int4 tail = p.tail[blockIdx.x];
-    if (tail.x < 0) return;
-    // The CTAs of all runs but the last one that have tiles of this sequence share the join: each takes some of the outputs, four values of
-    // a head an item, and some threads an item, which take some of the pieces (slot 1 of the first run, slot 0 of the others).  At most four
-    // threads an item: more shorten the walk over the pieces by less than the exchange at its end takes (B = 1, 1001 tokens: 8.3 us with
-    // sixteen, 7.9 with four).
-    const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * p.slots, nh = min(p.G - h0, p.slots);
-    const int n = tail.z - tail.y + 1, helpers = n - 1, helper = run - tail.y;
-    if (n < 2) return;
-    const int Dv = p.c.Dv, vecs = Dv / 4, all = nh * vecs;
-    const int item0 = all * helper / helpers, items = all * (helper + 1) / helpers - item0;
-    if (items == 0) return;
-    const int share = items >= kJoinThreads ? 1 : min(min(kJoinThreads / items, 4), n), at_once = kJoinThreads / share;
-    const int my = tid / share, part = tid - my * share;
-    const int64_t out0 = static_cast<int64_t>(tail.x) * p.Hq + hk * p.G + h0;
-    for (int base = 0; base < items; base += at_once) {
-      const bool on = my < at_once && base + my < items;
-      const int item = item0 + base + my, r = item / vecs, d = (item - r * vecs) * 4;
-      float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      float m = -INFINITY, l = 0.0f;
-      if (on) {                                  // maximum, sum and output together: one round trip to memory for four pieces
-        constexpr int kPieces = 4;
-        for (int i0 = part; i0 < n; i0 += share * kPieces) {
-          float2 ml[kPieces];
-          float4 x[kPieces];
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) {
-            const int i = i0 + k * share;
-            if (i < n) {
-              const int64_t s = ((static_cast<int64_t>(tail.y + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0)) * p.part_rows + r;
-              ml[k] = *reinterpret_cast<const float2*>(p.part_ml + s * 2);
-              x[k] = *reinterpret_cast<const float4*>(p.part + s * Dv + d);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) {
-            if (i0 + k * share < n) {
-              const float mn = fmaxf(m, ml[k].x);
-              const float a = m == -INFINITY ? 0.0f : ex2(m - mn), w = ml[k].x == -INFINITY ? 0.0f : ex2(ml[k].x - mn);
-              m = mn;
-              l = l * a + ml[k].y * w;
-              acc.x = acc.x * a + x[k].x * w;
-              acc.y = acc.y * a + x[k].y * w;
-              acc.z = acc.z * a + x[k].z * w;
-              acc.w = acc.w * a + x[k].w * w;
-            }
-          }
-        }
-      }
-      if (share > 1) {
-        __syncthreads();
-        sums[tid] = acc;
-        mls[tid] = make_float2(m, l);
-        __syncthreads();
-      }
-      if (on && part == 0) {
-        if (share > 1) {
-          for (int i = 1; i < share; ++i) m = fmaxf(m, mls[tid + i].x);
-          l = 0.0f;
-          acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int i = 0; i < share; ++i) {
-            const float2 ml = mls[tid + i];
-            const float w = ml.x == -INFINITY ? 0.0f : ex2(ml.x - m);
-            const float4 x = sums[tid + i];
-            l = fmaf(ml.y, w, l);
-            acc.x = fmaf(x.x, w, acc.x);
-            acc.y = fmaf(x.y, w, acc.y);
-            acc.z = fmaf(x.z, w, acc.z);
-            acc.w = fmaf(x.w, w, acc.w);
-          }
-        }
-        const float inv = 1.0f / l;
-        *reinterpret_cast<uint2*>(p.out + (out0 + r) * Dv + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-        if (d == 0 && p.lse) p.lse[out0 + r] = (m + log2f(l)) * 0.6931471805599453f;
-      }
-    }
+    join_tail<kJoinThreads>(p, threadIdx.x, 0, blockIdx.x % p.U, blockIdx.x / p.U, p.tail[blockIdx.x], sums, mls);
     return;
   }
-
   const int w = blockIdx.x - join_ctas, share = w % p.join_weight_ctas, bk = w / p.join_weight_ctas;
   const int b = bk / p.c.Hkv, hk = bk - b * p.c.Hkv;
   int2 span = p.seq_runs[b];                     // (anything at all for an empty sequence, and for one that has just stopped being one)
   span = make_int2(max(span.x, 0), min(span.y, p.runs - 1));
   const int L = seq_len(p, b);
-  if (L == 0 || static_cast<int64_t>(share) * kJoinThreads >= L) return;
-  for (int g = tid >> 5; g < p.G; g += kJoinThreads / 32) {
-    float lg;
-    if (span.x == span.y) {
-      lg = p.lse2[static_cast<int64_t>(b) * p.Hq + hk * p.G + g];
-    } else {
-      const int unit = hk * p.groups + g / p.slots, r = g % p.slots;
-      float m = -INFINITY, l = 0.0f;
-      for (int i = tid & 31; i <= span.y - span.x; i += 32) {
-        const int64_t slot = (static_cast<int64_t>(span.x + i) * p.U + unit) * 2 + (i == 0 ? 1 : 0);
-        const float2 x = *reinterpret_cast<const float2*>(p.part_ml + (slot * p.part_rows + r) * 2);
-        join_pair(m, l, x.x, x.y);
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, d), ol = __shfl_xor_sync(0xffffffffu, l, d);
-        join_pair(m, l, om, ol);
-      }
-      lg = m + log2f(l);
-    }
-    if ((tid & 31) == 0) lse2_sm[g] = lg;
-  }
-  __syncthreads();
-  constexpr int kAtOnce = 4;                     // positions of a thread whose loads are under way together
-  const int step = p.join_weight_ctas * kJoinThreads, first = share * kJoinThreads + tid;
-  const int64_t score_step = static_cast<int64_t>(step) * p.score_heads;
-  const float* s = p.scores + ((static_cast<int64_t>(b) * p.c.Hkv + hk) * p.score_ld + first) * p.score_heads;
-  float* out = p.weights + (static_cast<int64_t>(b) * p.c.Hkv + hk) * p.ld + first;
-  for (int left = L - first; left > 0; left -= step * kAtOnce, s += score_step * kAtOnce, out += static_cast<int64_t>(step) * kAtOnce) {
-    float acc[kAtOnce], was[kAtOnce];
-    const int n = min(kAtOnce, (left + step - 1) / step);        // positions of this thread
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      acc[i] = 0.0f;
-      if (i < n) was[i] = out[static_cast<int64_t>(i) * step];
-    }
-    if (p.score_heads == 4) {                    // (the ordinary number: one load a position)
-      float4 x[kAtOnce];
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i)
-        if (i < n) x[i] = __ldcg(reinterpret_cast<const float4*>(s + i * score_step));
-      const float l0 = lse2_sm[0], l1 = lse2_sm[1], l2 = lse2_sm[2], l3 = p.G > 3 ? lse2_sm[3] : INFINITY;
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i)
-        if (i < n) acc[i] = ex2(x[i].x - l0) + ex2(x[i].y - l1) + ex2(x[i].z - l2) + (l3 != INFINITY ? ex2(x[i].w - l3) : 0.0f);
-    } else {
-      for (int g = 0; g < p.G; g += 2) {
-        const float l0 = lse2_sm[g], l1 = g + 1 < p.G ? lse2_sm[g + 1] : INFINITY;      // (no weight for a head that is not there)
-        float2 x[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-          if (i < n) x[i] = __ldcg(reinterpret_cast<const float2*>(s + i * score_step + g));
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-          if (i < n) acc[i] += ex2(x[i].x - l0) + (l1 != INFINITY ? ex2(x[i].y - l1) : 0.0f);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-      if (i < n) out[static_cast<int64_t>(i) * step] = was[i] + acc[i];
-  }
+  if (static_cast<int64_t>(share) * kJoinThreads >= L) return;
+  add_weights<kJoinThreads>(p, threadIdx.x, b, hk, span, share * kJoinThreads, p.join_weight_ctas * kJoinThreads, L, lse2_sm);
 }
 
 struct PagedPlan {
@@ -966,17 +1034,28 @@ bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, Pag
   return true;
 }
 
-template <bool kInt8, int DP, int kHeads>
-msd_status_t launch_paged(const PagedAttnParams& p, cudaStream_t s) {
+template <bool kInt8, int DP, int kHeads, bool kJoin>
+bool launch_runs(const PagedAttnParams& p, cudaStream_t s, bool pdl) {
   using Sh = Shape<kInt8, DP, kHeads>;
-  auto kernel = attn_paged_kernel<kInt8, DP, kHeads>;
+  auto kernel = attn_paged_kernel<kInt8, DP, kHeads, kJoin>;
   static DeviceOnce once;
-  if (!once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem) == cudaSuccess; })) return MSD_ERR_CUDA;
+  if (!once([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem) == cudaSuccess &&
+               (!kJoin || cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess);
+      }))
+    return false;
+  if (launch_pdl_cluster(kernel, dim3(p.runs * p.U), dim3(Sh::kThreads), Sh::kSmem, s, pdl, kJoin ? p.runs : 1, p) == cudaSuccess) return true;
+  cudaGetLastError();
+  return false;
+}
+
+template <bool kInt8, int DP, int kHeads>
+msd_status_t launch_paged(const PagedAttnParams& p, bool cluster, cudaStream_t s) {
   const bool pdl = option(OPT_NO_PDL) != 1;
-  if (launch_pdl(kernel, dim3(p.runs * p.U), dim3(Sh::kThreads), Sh::kSmem, s, pdl, p) != cudaSuccess) {
-    cudaGetLastError();
-    return MSD_ERR_CUDA;
+  if constexpr (kHeads == 8) {
+    if (cluster) return launch_runs<kInt8, DP, kHeads, true>(p, s, pdl) ? MSD_OK : MSD_ERR_CUDA;
   }
+  if (!launch_runs<kInt8, DP, kHeads, false>(p, s, pdl)) return MSD_ERR_CUDA;
   if (p.runs == 1 && !p.weights) return MSD_OK;      // (every sequence was finished by one CTA)
   const unsigned weight_ctas = p.weights ? static_cast<unsigned>(p.B) * p.c.Hkv * p.join_weight_ctas : 0;
   if (launch_pdl(attn_paged_join_kernel, dim3(p.runs * p.U + weight_ctas), dim3(kJoinThreads), p.weights ? p.G * sizeof(float) : 0, s, pdl, p) !=
@@ -1010,8 +1089,9 @@ struct TileTokens {
 };
 struct Launch {
   const PagedAttnParams& p;
+  bool cluster;
   cudaStream_t s;
-  template <bool kInt8, int DP, int kHeads> msd_status_t operator()() const { return launch_paged<kInt8, DP, kHeads>(p, s); }
+  template <bool kInt8, int DP, int kHeads> msd_status_t operator()() const { return launch_paged<kInt8, DP, kHeads>(p, cluster, s); }
 };
 
 }  // namespace
@@ -1081,6 +1161,13 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.U = pl.U;
   // no more runs than tiles that the sequences have room for (their lengths are on the device)
   p.runs = room < pl.runs ? static_cast<int>(room) : pl.runs;
+  bool cluster = false;
+  if (slots == 8) {
+    int runs = 1;
+    while (runs < room && runs * 2 <= pl.runs && runs < kClusterCtas) runs *= 2;
+    cluster = room <= runs * kClusterTiles;
+    if (cluster) p.runs = runs;
+  }
   p.scale2 = softmax_scale * 1.4426950408889634f;
   p.out = static_cast<uint16_t*>(out_bf16);
   p.lse = lse;
@@ -1100,7 +1187,7 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   const int64_t most = (ld + kJoinThreads - 1) / kJoinThreads, fill = (4LL * sm_count() + static_cast<int64_t>(B) * cache->Hkv - 1) / (static_cast<int64_t>(B) * cache->Hkv);
   p.join_weight_ctas = static_cast<int>(most < fill ? (most < 1 ? 1 : most) : fill);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return with_shape(int8, widest, slots, Launch{p, s});
+  return with_shape(int8, widest, slots, Launch{p, cluster, s});
 }
 
 }  // extern "C"

@@ -25,7 +25,8 @@
 // Split over the length: the tiles of all sequences form one list, cut into equal runs; run i is walked by U = KV heads x head groups
 // CTAs side by side, one per unit, so that CTAs that run together read neighbouring rows.  The grid is what is resident at once.
 // A sequence inside one run is finished there; only the first and the last of a run can be cut, so a CTA leaves at most two
-// partial results, whatever the lengths are, and a second kernel joins those and turns the scores into weights.
+// partial results, whatever the lengths are, and a second kernel joins those and turns the scores into weights.  With few tiles the runs of a
+// unit are a cluster, which joins them and adds the weights itself after a barrier: one launch.
 //
 // Tried and dropped: the last CTA to leave a partial result of a sequence joins them (registers of the tile loop; 32 x 2048-8192
 // tokens 122 -> 124 us at best, one of 1001 10.1 -> 9.0); keys and values asked for one by one as soon as their halves of a stage are free
@@ -45,7 +46,7 @@ namespace {
 constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
 constexpr int kAtOnceWeights = 4;           // positions of a thread whose scores are under way together
-constexpr int kClusterTiles = 4, kClusterCtas = 16;
+constexpr int kClusterTiles = 4, kClusterCtas = 16;     // one kernel: most tiles of a CTA, most CTAs of a unit
 constexpr float kHeld = 8.0f;               // how far (log2) a score may exceed its reference before that moves
 constexpr float kPUnits = 128.0f;           // INT8: 2^15 / 2^kHeld
 
@@ -411,6 +412,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   if (threadIdx.x == 0) *tail = make_int4(-1, 0, 0, 0);
   const int runs = min(p.runs, T);                // (no empty runs)
   auto meet_cluster = [&]() {                     // every CTA of the unit is done; the rings are free
+    int some = lane < p.B ? seq_len(p, lane) : 0;           // 32 lengths
     cluster_arrive_all();
     cluster_wait_all();
     float4* sums = reinterpret_cast<float4*>(smem);
@@ -419,20 +421,21 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     constexpr int kHalf = S::kThreads / 2;        // half of the warps join while the others add weights
     if (threadIdx.x < kHalf) join_tail<kHalf>(p, threadIdx.x, 1, unit, run, tail_sm, sums, mls);
     if (threadIdx.x < kHalf || !p.weights) return;
-    // (blocks of positions, dealt out to the warps of all CTAs sequence after sequence)
+    // (blocks of positions, dealt out in turn to the warps of all CTAs, sequence after sequence)
     constexpr int kBlock = 32 * kAtOnceWeights, kAdders = S::kWarps - S::kWarps / 2;
     const int adders = p.runs * kAdders, adder = run * kAdders + warp - S::kWarps / 2;
     lse2_sm += warp * 8;
-    int64_t at = 0;
-    int turn = 0;
-    for (int b = 0; b < p.B && T > 0; ++b) {
-      const int L = seq_len(p, b), blocks = (L + kBlock - 1) / kBlock;
-      const int64_t upto = at + (L + S::kTile - 1) / S::kTile;
-      const int run0 = static_cast<int>(((at + 1) * runs - 1) / T), run1 = min(static_cast<int>((upto * runs - 1) / T), runs - 1);
-      for (int i = adder >= turn ? adder - turn : adder - turn + adders; i < blocks; i += adders)
-        add_weights<32>(p, lane, b, hk, make_int2(run0, run1), i * kBlock, 32, min(L, (i + 1) * kBlock), lse2_sm);
+    int at = 0, turn = adder;                     // tiles of the sequences before this one; this warp's first block of it
+    for (int b = 0; b < p.B; ++b) {
+      if (b != 0 && b % 32 == 0) some = b + lane < p.B ? seq_len(p, b + lane) : 0;
+      const int L = __shfl_sync(0xffffffffu, some, b % 32), upto = at + (L + S::kTile - 1) / S::kTile;
+      for (; turn * kBlock < L; turn += adders) {
+        // (there are few tiles: 32 bits will do)
+        const int2 span = make_int2(((at + 1) * runs - 1) / T, min((upto * runs - 1) / T, runs - 1));
+        add_weights<32>(p, lane, b, hk, span, turn * kBlock, 32, min(L, (turn + 1) * kBlock), lse2_sm);
+      }
+      turn -= (L + kBlock - 1) / kBlock;
       at = upto;
-      turn = (turn + blocks) % adders;
     }
   };
   if (run >= runs) {
@@ -1117,7 +1120,8 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   const bool int8 = cache->type == MSD_CACHE_INT8;
   const int widest = cache->D > cache->Dv ? cache->D : cache->Dv, slots = Hq / cache->Hkv <= 8 ? 8 : kMaxSlots;
   PagedPlan pl;
-  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, with_shape(int8, widest, slots, CtasPerSm{}), &pl)) return MSD_ERR_UNSUPPORTED;
+  const int ctas_per_sm = with_shape(int8, widest, slots, CtasPerSm{});
+  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, ctas_per_sm, &pl)) return MSD_ERR_UNSUPPORTED;
   if (!q_bf16 || !block_table || !seqlens || !out_bf16 || !workspace) return MSD_ERR_NULL_POINTER;
   if (!aligned(q_bf16, 16) || q_ld % 8 != 0 || !aligned(out_bf16, 16) || !aligned(workspace, 1024) || !aligned(block_table, 4) ||
       !aligned(seqlens, 4) || !aligned(lse, 4) || !aligned(weights, 4))
@@ -1129,11 +1133,11 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
     return MSD_ERR_UNSUPPORTED;
   // (positions stay below 2^31 - the tokens of a tile, and tiles below 2^31, so that no sum of theirs wraps)
   p.cap = static_cast<int64_t>(max_blocks) * cache->page_size;
-  if (weights && p.cap > ld) p.cap = ld;
   if (p.cap > 0x7FFFF000) p.cap = 0x7FFFF000;
   const int tile = with_shape(int8, widest, slots, TileTokens{});
-  const int64_t room = (p.cap + tile - 1) / tile * B;
+  const int64_t room = (p.cap + tile - 1) / tile * B;      // tiles; of the table alone: the schedule, and so the bits, do not depend on the weights
   if (room > 0x7FFFFFFF) return MSD_ERR_UNSUPPORTED;
+  if (weights && p.cap > ld) p.cap = ld;
   p.k_block = static_cast<uint32_t>(p.c.k.block / 16);
   p.k_token = static_cast<uint32_t>(p.c.k.token / 16);
   p.v_block = static_cast<uint32_t>(p.c.v.block / 16);
@@ -1161,11 +1165,17 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.U = pl.U;
   // no more runs than tiles that the sequences have room for (their lengths are on the device)
   p.runs = room < pl.runs ? static_cast<int>(room) : pl.runs;
+  // Few tiles: one kernel, in which the runs of a unit are a cluster.  It saves a launch and the second kernel's first loads, but has at most 16
+  // runs; so a CTA has no more tiles than in the other form, or up to four of a single sequence (a second sequence costs more than a second
+  // tile).  32/8 heads of 128 on the GPU, two kernels / one: BF16 1 x 1000 tokens 8.0 / 6.9 us, 1 x 4000 13.1 / 9.7, 4 x 128-256 with weights 7.8 /
+  // 7.1, INT8 1 x 4000 with weights 11.9 / 10.4, 8 x 128-256 9.3 / 8.4; 16 x 32-64 with weights 6.9 / 7.5.  The call's host time goes from 6.4 to 4.2 us.
   bool cluster = false;
   if (slots == 8) {
     int runs = 1;
-    while (runs < room && runs * 2 <= pl.runs && runs < kClusterCtas) runs *= 2;
-    cluster = room <= runs * kClusterTiles;
+    const int most = ctas_per_sm == 1 ? kClusterCtas / 2 : kClusterCtas;        // (a cluster lies on the SMs of one GPC)
+    while (runs < room && runs * 2 <= pl.runs && runs < most) runs *= 2;
+    const int64_t tiles = (room + pl.runs - 1) / pl.runs;        // of a CTA in the other form
+    cluster = room <= runs * (B == 1 ? kClusterTiles : (tiles < kClusterTiles ? tiles : kClusterTiles));
     if (cluster) p.runs = runs;
   }
   p.scale2 = softmax_scale * 1.4426950408889634f;

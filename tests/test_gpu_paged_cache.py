@@ -124,6 +124,35 @@ def test_attention_with_every_width_of_a_row(D, Dv, G, int8):
     _check_attention(q, c, D ** -0.5, out, lse, before, weights)
 
 
+# calls with so few tiles that one kernel does everything, and their neighbours: (lengths, Hq, Hkv, D, Dv)
+FEW = [([4000], 32, 8, 128, 128), ([4200], 32, 8, 128, 128), ([2049], 7, 1, 64, 64), ([65], 16, 16, 80, 80), ([1500], 4, 2, 256, 192), ([129], 3, 1, 192, 192),
+       ([100, 0, 64, 17, 128], 10, 2, 128, 128), ([0, 1, 2, 3, 70, 5, 0, 40], 24, 8, 64, 64), ([33, 250], 32, 32, 128, 64), ([0, 0], 4, 4, 64, 64),
+       ([1] * 16, 8, 8, 128, 128), ([(7 * i) % 61 for i in range(40)], 54, 27, 64, 64)]
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lengths,Hq,Hkv,D,Dv", FEW)
+def test_attention_over_few_tiles(lengths, Hq, Hkv, D, Dv, int8):
+    B, ld = len(lengths), max(max(lengths), 1)
+    c = make_cache(lengths, Hkv, D, Dv, 16, int8, seed=sum(lengths))
+    q = torch.randn(B, Hq, D, generator=torch.Generator().manual_seed(D)).to(torch.bfloat16).cuda()
+    before = torch.rand(B, Hkv, ld, generator=torch.Generator().manual_seed(B)).cuda()
+    got = []
+    for no_pdl in (-1, 1):
+        binding.debug_set_option("MSD_NO_PDL", no_pdl)
+        ws = binding.workspace(binding.attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld))
+        for _ in range(2):
+            ws.fill_(255)
+            weights = before.clone()
+            got.append(binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True, ws=ws) + (weights,))
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, *got[0][:2], before, got[0][2])
+    for other in got[1:]:
+        for x, y in zip(got[0], other):
+            assert torch.equal(x, y)
+    assert torch.equal(binding.attn_decode_paged(q, *_args(c), D ** -0.5), got[0][0])
+
+
 def test_attention_with_more_heads_than_places_on_the_machine():
     """Every CTA walks all sequences of its KV head; one query head each, and 8 groups of 16 for the others."""
     for Hq, Hkv in ((900, 900), (640, 5)):

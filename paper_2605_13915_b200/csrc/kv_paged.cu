@@ -193,7 +193,7 @@ msd_status_t launch_append(const AppendParams& p, cudaStream_t s) {
 // is the next range.  (Cutting the range that is there, not the whole range of the bits, spreads the first histogram over more bins: threads
 // that add to the same one wait for each other.)  What is above the k-th stays, of what
 // equals it the first ones; a scan over the positions in order gives each its new place.  (Finding it by two bits a round, three counts
-// over all keys: 61 instead of 17 us for 256 rows of 2048 to 8192.  The peers' histograms read, not added to by atomics: 8 rows of 131072
+// over all keys: 61 instead of 17 us for 256 rows of 2048 to 8192, which are 16 since keys are walked four at a time.  The peers' histograms read, not added to by atomics: 8 rows of 131072
 // 48 -> 52 us, the move included.)
 // ---------------------------------------------------------------------------------------------------------------------------
 struct EvictParams {
@@ -290,8 +290,11 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int cluster_ctas) 
   auto for_keys = [&](auto&& f) {                       // (alike in all lanes)
     if constexpr (kKeys > 0) {
 #pragma unroll
-      for (int j = 0; j < kKeys; ++j)
-        if (j < rows) f(j, key[j]);
+      for (int j0 = 0; j0 < kKeys; j0 += 4) {           // (key[j] is 0, which counts nowhere, from `rows` on)
+        if (j0 >= rows) break;
+#pragma unroll
+        for (int j = j0; j < j0 + 4; ++j) f(j, key[j]);
+      }
     } else {
 #pragma unroll 4
       for (int j = 0; j < rows; ++j) f(j, key_at(j));
@@ -433,15 +436,23 @@ kv_evict_select_kernel(const __grid_constant__ EvictParams p, int cluster_ctas) 
   if constexpr (kKeys > 0) {
     float x[kKeys];
 #pragma unroll
-    for (int j = 0; j < kKeys; ++j) {
-      key[j] = j < rows ? place(key[j]) : kNowhere;
-      x[j] = key[j] != kNowhere ? w_lane[j * 32] : 0.0f;
+    for (int j0 = 0; j0 < kKeys; j0 += 4) {
+      if (j0 >= rows) break;
+#pragma unroll
+      for (int j = j0; j < j0 + 4; ++j) {
+        key[j] = place(key[j]);
+        x[j] = key[j] != kNowhere ? w_lane[j * 32] : 0.0f;
+      }
     }
 #pragma unroll
-    for (int j = 0; j < kKeys; ++j) {
-      if (key[j] == kNowhere) continue;
-      kept[key[j]] = static_cast<int32_t>(begin + j * 32);
-      new_w[key[j]] = x[j];
+    for (int j0 = 0; j0 < kKeys; j0 += 4) {
+      if (j0 >= rows) break;
+#pragma unroll
+      for (int j = j0; j < j0 + 4; ++j) {
+        if (key[j] == kNowhere) continue;
+        kept[key[j]] = static_cast<int32_t>(begin + j * 32);
+        new_w[key[j]] = x[j];
+      }
     }
   } else {
     for (int j = 0; j < rows; ++j) {

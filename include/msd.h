@@ -403,6 +403,7 @@ void msd_debug_set_attn_dump(int8_t* q_dbg, float* q_scale_dbg, int32_t* s_dbg);
  * A length below 0 or above what the call has room for, or an entry outside [0, num_blocks), is reported as MSD_ERR_BAD_SHAPE by
  * msd_last_device_status; the results of that sequence are then unspecified, but nothing outside the buffers is touched.
  * A page may be listed by several sequences (a shared prefix) where it is read only.
+ * As for all device arrays of this library, lengths, tables and weights stay as they are while a call that reads them runs.
  */
 typedef enum { MSD_CACHE_BF16 = 0, MSD_CACHE_INT8 = 1 } msd_cache_type_t;
 typedef struct {

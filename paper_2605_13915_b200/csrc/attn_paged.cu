@@ -374,6 +374,9 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   __shared__ float ml[3][S::kWarps][kHeads];              // of a warp: references, sums, units of its outputs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   __shared__ int4 tail_sm;                               // (kJoin)
+  // kJoin: the lengths, read once, so that all warps walk alike and meet at their barriers whatever becomes of the lengths meanwhile.  (Otherwise
+  // a warp that is done leaves, and no barrier waits for it.)
+  __shared__ int lengths[kJoin ? kClusterTiles * kClusterCtas : 1];
   const int unit = kJoin ? blockIdx.x / p.runs : blockIdx.x % p.U, run = kJoin ? blockIdx.x % p.runs : blockIdx.x / p.U;
   const int hk = unit / p.groups, h0 = (unit - hk * p.groups) * kHeads;        // first head of the group within the KV head
   const int nh = min(p.G - h0, kHeads);
@@ -383,13 +386,17 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   pdl_launch_dependents();
 
   // ---- this CTA's run of tiles ----  (every warp by itself; a lane looks at a share of the sequences)
+  if constexpr (kJoin) {
+    for (int b = threadIdx.x; b < p.B; b += S::kThreads) lengths[b] = seq_len(p, b);
+    __syncthreads();
+  }
+  auto len_of = [&](int b) { return kJoin ? lengths[b] : seq_len(p, b); };
   const int per_lane = (p.B + 31) / 32, b_lo = min(p.B, lane * per_lane), b_hi = min(p.B, b_lo + per_lane);
   int mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
-    const int32_t n = p.seqlens[b];
-    const int L = static_cast<int>(min(static_cast<int64_t>(max(n, 0)), p.cap));
+    const int L = len_of(b);
     if (warp == 0) {
-      if (L != n && blockIdx.x == 0) atomicMax(p.status, kStatusBadShape);
+      if (blockIdx.x == 0 && L != p.seqlens[b]) atomicMax(p.status, kStatusBadShape);
       if (L == 0 && b % p.runs == run) {         // nothing to attend to
         for (int h = 0; h < nh; ++h) {
           const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + h;
@@ -412,7 +419,6 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   if (threadIdx.x == 0) *tail = make_int4(-1, 0, 0, 0);
   const int runs = min(p.runs, T);                // (no empty runs)
   auto meet_cluster = [&]() {                     // every CTA of the unit is done; the rings are free
-    int some = lane < p.B ? seq_len(p, lane) : 0;           // 32 lengths
     cluster_arrive_all();
     cluster_wait_all();
     float4* sums = reinterpret_cast<float4*>(smem);
@@ -427,8 +433,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
     lse2_sm += warp * 8;
     int at = 0, turn = adder;                     // tiles of the sequences before this one; this warp's first block of it
     for (int b = 0; b < p.B; ++b) {
-      if (b != 0 && b % 32 == 0) some = b + lane < p.B ? seq_len(p, b + lane) : 0;
-      const int L = __shfl_sync(0xffffffffu, some, b % 32), upto = at + (L + S::kTile - 1) / S::kTile;
+      const int L = lengths[b], upto = at + (L + S::kTile - 1) / S::kTile;
       for (; turn * kBlock < L; turn += adders) {
         // (there are few tiles: 32 bits will do)
         const int2 span = make_int2(((at + 1) * runs - 1) / T, min((upto * runs - 1) / T, runs - 1));
@@ -448,7 +453,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   int b_first = b_lo, t_first = first - before;
   if (here) {
     for (; b_first + 1 < b_hi; ++b_first) {
-      const int t = (seq_len(p, b_first) + S::kTile - 1) / S::kTile;
+      const int t = (len_of(b_first) + S::kTile - 1) / S::kTile;
       if (t_first < t) break;
       t_first -= t;
     }
@@ -464,14 +469,14 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
   Walk ld;
   ld.b = b_first;
   ld.tile = t_first;
-  ld.L = seq_len(p, ld.b);
+  ld.L = len_of(ld.b);
   ld.tiles = (ld.L + S::kTile - 1) / S::kTile;
   ld.left = end - first;
   Walk cur = ld;
   auto next_sequence = [&](Walk& w) {
     do {                                      // (there is one, unless the lengths are changed meanwhile)
       w.b = min(w.b + 1, p.B - 1);
-      w.L = seq_len(p, w.b);
+      w.L = len_of(w.b);
     } while (w.L == 0 && w.b + 1 < p.B);
     w.tile = 0;
     w.tiles = (w.L + S::kTile - 1) / S::kTile;

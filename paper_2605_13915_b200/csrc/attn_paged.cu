@@ -43,7 +43,6 @@ namespace msd {
 
 namespace {
 
-constexpr int kMaxSlots = 16;               // head slots of a CTA: 8 where a KV head has up to 8 query heads, else 16
 constexpr int kJoinThreads = 256;
 constexpr int kAtOnceWeights = 4;           // positions of a thread whose scores are under way together
 constexpr int kClusterTiles = 4, kClusterCtas = 16;     // one kernel: most tiles of a CTA, most CTAs of a unit
@@ -66,7 +65,7 @@ struct PagedAttnParams {
   float* weights;
   int64_t ld, score_ld;
   int score_heads;            // heads of a position's scores: G, made even
-  int slots;                  // head slots of a CTA, 8 or 16
+  int slots;                  // head slots of a CTA, 8, 16 or 24
   // workspace
   float* part;                // [CTA][2][rows][Dv]: unnormalised outputs
   float* part_ml;             // [CTA][2][rows][2]: maximum (log2) and sum
@@ -139,7 +138,7 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
   return *reinterpret_cast<const uint32_t*>(&d);
 }
 
-// DP: D and Dv rounded up to 64, 96, 128, 192 or 256; kHeads: head slots of a CTA, 8 or 16.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB
+// DP: D and Dv rounded up to 64, 96, 128, 192 or 256; kHeads: head slots of a CTA, 8, 16 or 24.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB
 // of keys and values; the rings of an SM's CTAs hold 140 to 200 KB.  Two stages and as many warps as their registers allow (heads of 128, 32 x
 // 2048-8192 tokens: INT8 81 / 85 us, 16 / 16 heads of 80 52 / 57 with more stages and fewer warps; at the same number of warps a third
 // stage, 24 x 1024-4096: 16 / 16 heads of 64 INT8 39.9 / 44.0, of 256 99 / 101), but for BF16 with two CTAs an SM (128 / 8 heads of 128: 53.5 with two
@@ -155,11 +154,12 @@ struct Shape {
   static constexpr int kHalf = kTok * kRow;                     // keys, then values
   static constexpr int kScale = kInt8 ? kTok * 4 : 0;           // then the scales of both
   static constexpr int kStage = 2 * kHalf + 2 * kScale;
-  static constexpr int kCtasPerSm = !kInt8 && DP == 256  ? 1
+  static constexpr int kCtasPerSm = kHeads == 24         ? 2
+                                    : !kInt8 && DP == 256 ? 1
                                     : kInt8 && DP == 64  ? (kHeads == 8 ? 4 : 3)
                                     : DP == 96 || (kHeads == 8 && DP <= (kInt8 ? 192 : 128)) ? 3
                                                          : 2;
-  static constexpr bool kQInSmem = DP == 256 && kHeads == 16;   // (64 registers of query fragments beside 128 of outputs are too many)
+  static constexpr bool kQInSmem = (DP == 256 && kHeads == 16) || (DP >= 128 && kHeads == 24);   // (the registers of the outputs leave it no room)
   static constexpr int kQBytes = kQInSmem ? (DP / 16) * (kHeads / 8) * 32 * 8 : 0, kStatic = 2304;
   static constexpr int kStages = !kInt8 && kCtasPerSm == 2 && 2 * kWarps * 3 * kStage <= 200 * 1024 ? 3 : 2;
   static constexpr int kRing = kWarps * kStages * kStage;
@@ -1013,12 +1013,20 @@ struct PagedPlan {
   size_t part, ml, tail, seq_runs, lse2, scores, bytes;     // offsets into the workspace
 };
 
+// Head slots of a CTA: 8 for up to 8 query heads of a KV head, else 16, or 24 where that makes fewer groups of them and rows are not too wide for
+// its registers (each group reads the cache and converts it: 160 / 8 heads of 128, 32 x 2048-8192 tokens BF16 188 -> 128 us, INT8
+// 156 -> 107; of 192 280 -> 191, 232 -> 197).
+int head_slots(int G, int widest) {
+  if (G <= 8) return 8;
+  return widest <= 192 && (G + 23) / 24 < (G + 15) / 16 ? 24 : 16;
+}
+
 // (ctas_per_sm: 4, the most of any kernel, where the head dimension is not known; the workspace has room for that)
-bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int ctas_per_sm, PagedPlan* pl) {
+bool plan_paged(int B, int Hq, int Hkv, int Dv, int64_t ld, int slots, int ctas_per_sm, PagedPlan* pl) {
   if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 8192 || B > (1 << 20) || Dv < 1 || Dv > 256 || ld < 0 || ld > 0x7FFFFFFF) return false;
   if (static_cast<int64_t>(B) * Hkv > (1 << 24) || static_cast<double>(B) * (Hq + Hkv) * ld > 1e15) return false;      // (grids and sizes that count)
   const int G = Hq / Hkv;
-  pl->slots = G <= 8 ? 8 : kMaxSlots;
+  pl->slots = slots;
   pl->groups = (G + pl->slots - 1) / pl->slots;
   pl->U = Hkv * pl->groups;
   pl->runs = sm_count() * ctas_per_sm / pl->U;
@@ -1078,6 +1086,9 @@ msd_status_t launch_paged(const PagedAttnParams& p, bool cluster, cudaStream_t s
 template <typename F>
 auto with_shape(bool int8, int widest, int slots, F&& f) {
   auto heads = [&](auto i8, auto dp) {
+    if constexpr (decltype(dp)::value <= 192) {
+      if (slots == 24) return f.template operator()<decltype(i8)::value, decltype(dp)::value, 24>();
+    }
     return slots == 8 ? f.template operator()<decltype(i8)::value, decltype(dp)::value, 8>() : f.template operator()<decltype(i8)::value, decltype(dp)::value, 16>();
   };
   auto size = [&](auto i8) {
@@ -1109,8 +1120,13 @@ struct Launch {
 extern "C" {
 
 size_t msd_attn_decode_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Dv, int64_t ld) {
-  msd::PagedPlan pl;
-  return msd::plan_paged(B, Hq, Hkv, Dv, ld, 4, &pl) ? pl.bytes : 0;
+  size_t most = 0;                              // of the kernels that a size of the keys may choose
+  for (int widest : {192, 256}) {
+    msd::PagedPlan pl;
+    if (!msd::plan_paged(B, Hq, Hkv, Dv, ld, msd::head_slots(Hkv < 1 ? 1 : Hq / Hkv, widest), 4, &pl)) return 0;
+    if (pl.bytes > most) most = pl.bytes;
+  }
+  return most;
 }
 
 msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_paged_cache_t* cache, const int32_t* block_table,
@@ -1123,10 +1139,10 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   if (q_ld < static_cast<int64_t>(Hq) * cache->D) return MSD_ERR_BAD_SHAPE;
   if (B == 0) return MSD_OK;
   const bool int8 = cache->type == MSD_CACHE_INT8;
-  const int widest = cache->D > cache->Dv ? cache->D : cache->Dv, slots = Hq / cache->Hkv <= 8 ? 8 : kMaxSlots;
+  const int widest = cache->D > cache->Dv ? cache->D : cache->Dv, slots = head_slots(Hq / cache->Hkv, widest);
   PagedPlan pl;
   const int ctas_per_sm = with_shape(int8, widest, slots, CtasPerSm{});
-  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, ctas_per_sm, &pl)) return MSD_ERR_UNSUPPORTED;
+  if (!plan_paged(B, Hq, cache->Hkv, cache->Dv, weights ? ld : 0, slots, ctas_per_sm, &pl)) return MSD_ERR_UNSUPPORTED;
   if (!q_bf16 || !block_table || !seqlens || !out_bf16 || !workspace) return MSD_ERR_NULL_POINTER;
   if (!aligned(q_bf16, 16) || q_ld % 8 != 0 || !aligned(out_bf16, 16) || !aligned(workspace, 1024) || !aligned(block_table, 4) ||
       !aligned(seqlens, 4) || !aligned(lse, 4) || !aligned(weights, 4))

@@ -124,6 +124,21 @@ def test_attention_with_every_width_of_a_row(D, Dv, G, int8):
     _check_attention(q, c, D ** -0.5, out, lse, before, weights)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D,Dv", [(64, 64), (80, 96), (128, 112), (128, 192), (256, 64)])
+@pytest.mark.parametrize("G", [17, 20, 24, 25, 40])
+def test_attention_with_many_heads_to_a_kv_head(G, D, Dv, int8):
+    """17 to 24 heads are one group of a CTA's slots, 33 to 48 two, where rows are not wider than 192."""
+    c = make_cache([450, 0, 31, 129], 2, D, Dv, 16, int8, seed=G)
+    q = torch.randn(4, 2 * G, D, generator=torch.Generator().manual_seed(G)).to(torch.bfloat16).cuda()
+    before = torch.rand(4, 2, 450, generator=torch.Generator().manual_seed(D)).cuda()
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+    assert torch.equal(binding.attn_decode_paged(q, *_args(c), D ** -0.5), out)
+
+
 # calls with so few tiles that one kernel does everything, and their neighbours: (lengths, Hq, Hkv, D, Dv)
 FEW = [([4000], 32, 8, 128, 128), ([4200], 32, 8, 128, 128), ([2049], 7, 1, 64, 64), ([65], 16, 16, 80, 80), ([1500], 4, 2, 256, 192), ([129], 3, 1, 192, 192),
        ([100, 0, 64, 17, 128], 10, 2, 128, 128), ([0, 1, 2, 3, 70, 5, 0, 40], 24, 8, 64, 64), ([33, 250], 32, 32, 128, 64), ([0, 0], 4, 4, 64, 64),

@@ -142,7 +142,7 @@ def test_attention_with_many_heads_to_a_kv_head(G, D, Dv, int8):
 # calls with so few tiles that one kernel does everything, and their neighbours: (lengths, Hq, Hkv, D, Dv)
 FEW = [([4000], 32, 8, 128, 128), ([4200], 32, 8, 128, 128), ([2049], 7, 1, 64, 64), ([65], 16, 16, 80, 80), ([1500], 4, 2, 256, 192), ([129], 3, 1, 192, 192),
        ([100, 0, 64, 17, 128], 10, 2, 128, 128), ([0, 1, 2, 3, 70, 5, 0, 40], 24, 8, 64, 64), ([33, 250], 32, 32, 128, 64), ([0, 0], 4, 4, 64, 64),
-       ([1] * 16, 8, 8, 128, 128), ([(7 * i) % 61 for i in range(40)], 54, 27, 64, 64)]
+       ([1] * 16, 8, 8, 128, 128), ([1800], 32, 2, 128, 128), ([70, 3], 9, 1, 256, 256), ([500], 24, 2, 80, 192), ([0, 64, 200], 26, 2, 64, 64), ([(7 * i) % 61 for i in range(40)], 54, 27, 64, 64)]
 
 
 @pytest.mark.parametrize("int8", [False, True])

@@ -422,7 +422,8 @@ typedef struct {
  *   k_new [n_rows, Hkv, D], v_new [n_rows, Hkv, Dv] BF16, 16-byte aligned, rows k_ld / v_ld elements apart (multiples of 8, so they may
  *   be slices of a projection's result); cu_new [B+1] INT32 (device), not falling; rows from cu_new[B] on (padding) are left out.
  * BF16 caches: copied.  INT8 caches, per row: scale = max|x| / 127, code = clamp(rne(x / scale), -127, 127), in IEEE FP32 with
- * true divisions; a zero row gives scale 0 and codes 0.
+ * true divisions; a zero row gives scale 0 and codes 0, a row with a NaN scale NaN and codes 0, one with an infinity and no NaN scale
+ * infinity and codes 0 (what is read back is then no number).
  *   weights nullable [B, Hkv, ld] FP32: the accumulated weights of msd_attn_decode_paged; those of the new positions are set to 0.
  * No position may be written by two rows: a page that this call writes is listed by one sequence.
  */

@@ -77,14 +77,14 @@ __device__ __forceinline__ uint2 codes_of(const uint4& v, float s, float inv) {
   return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
                     __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
 }
-// The same for a row whose largest value is tiny or huge (or no number), by true divisions.
+// The same for a row whose largest value is tiny or huge, by true divisions, or no finite number: then the scale tells of it and the codes are 0.
 __device__ __noinline__ uint2 codes_by_division(uint4 v, float s) {
   uint32_t w[4] = {v.x, v.y, v.z, v.w};
   unsigned long long out = 0;
 #pragma unroll 1
   for (int e = 0; e < 8; ++e) {
     int c = 0;
-    if (s > 0.0f) c = max(-127, min(127, __float2int_rn(__fdiv_rn(bf16lo(w[0]), s))));
+    if (s > 0.0f && s < INFINITY) c = max(-127, min(127, __float2int_rn(__fdiv_rn(bf16lo(w[0]), s))));
     out |= static_cast<unsigned long long>(c & 0xFF) << (8 * e);
     w[0] = __funnelshift_r(w[0], w[1], 16); w[1] = __funnelshift_r(w[1], w[2], 16); w[2] = __funnelshift_r(w[2], w[3], 16); w[3] >>= 16;
   }
@@ -149,11 +149,12 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
             if (d < D) *reinterpret_cast<uint4*>(to + d * 2) = x[a][i];
           }
         } else {
-          float m = 0.0f;
+          uint32_t top = 0;                              // (as bits, where a NaN is above infinity: a maximum of floats would drop it)
 #pragma unroll
-          for (int i = 0; i < kVecs; ++i) m = fmaxf(m, unit_absmax(x[a][i]));
+          for (int i = 0; i < kVecs; ++i) top = max(top, __float_as_uint(unit_absmax(x[a][i])));
 #pragma unroll
-          for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const float m = __uint_as_float(top);
           float s = by_127(m), inv;
           const bool plain = m > 1e-28f && m < 1e32f;
           if (!plain) s = __fdiv_rn(m, 127.0f);

@@ -467,6 +467,58 @@ def test_append_quantises_every_pair_of_significands():
         assert torch.equal(got.cpu(), ref)
 
 
+@pytest.mark.parametrize("what", ["nan", "inf", "-inf", "nan and inf", "only nan"])
+@pytest.mark.parametrize("D,Dv", [(64, 64), (128, 112), (256, 144)])
+def test_append_passes_on_what_is_no_finite_number(D, Dv, what):
+    """A NaN or an infinity in a row of an INT8 cache: alone in its 16 bytes, beside the row's largest finite value, in the last piece of
+    the row (the second one of its lane where rows are wide), in a key or in a value.  The row's scale tells of it and its codes are 0;
+    all other rows are what they would be."""
+    g = torch.Generator().manual_seed(D)
+    n, Hkv = 24, 3
+    new = {"k": torch.randn(n, Hkv, D, generator=g).to(torch.bfloat16), "v": torch.randn(n, Hkv, Dv, generator=g).to(torch.bfloat16)}
+    bad = {x: torch.zeros(n, Hkv, dtype=torch.bool) for x in new}
+    for i in range(0, n, 2):
+        x, h = "kv"[i // 2 % 2], i // 4 % Hkv
+        row = new[x][i, h]
+        at = (0, 9, len(row) - 8, len(row) - 1, len(row) // 2)[i // 2 % 5]
+        if i % 3 == 0:
+            row[at ^ 1] = 300.0                                   # in the same 16 bytes
+        if what == "only nan":
+            row[:] = float("nan")
+        else:
+            row[at] = float(what.split()[0])
+            if what == "nan and inf":
+                row[(at + 16) % len(row)] = float("inf")
+        bad[x][i, h] = True
+    c = make_cache([n], Hkv, D, Dv, 16, int8=True, poison=False)
+    finite = {x: torch.where(bad[x][..., None], torch.zeros_like(new[x]), new[x]) for x in new}
+    want = _append_reference(c, finite["k"], finite["v"], [0, n])
+    binding.kv_append_paged(new["k"].cuda(), new["v"].cuda(), *_args(c), torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    binding.last_device_status()
+    pos, table = torch.arange(n), c["table"].cpu()
+    for x, codes, scales, ref_codes, ref_scales in (("k", c["k"], c["k_scale"], want[0], want[2]), ("v", c["v"], c["v_scale"], want[1], want[3])):
+        assert torch.equal(codes.cpu(), ref_codes), x             # (zeros in the rows that are no numbers)
+        scales, ref_scales = (s.cpu()[table[0, pos // 16].long(), pos % 16] for s in (scales, ref_scales))
+        assert torch.equal(scales[~bad[x]].view(torch.int32), ref_scales[~bad[x]].view(torch.int32)), x
+        none = scales[bad[x]]
+        assert (none.isnan() if "nan" in what else none == float("inf")).all(), x
+
+
+def test_attention_over_appended_rows_that_are_no_numbers():
+    """What an INT8 cache was given as NaN comes out as NaN, as from a BF16 cache, and only from the KV head that was given it."""
+    new = torch.randn(2, 40, 2, 64, generator=torch.Generator().manual_seed(31)).to(torch.bfloat16).cuda()
+    new[0, 7, 1, 3] = new[1, 30, 0, 60] = float("nan")
+    cu = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+    q = torch.randn(1, 4, 64, generator=torch.Generator().manual_seed(32)).to(torch.bfloat16).cuda()
+    for int8 in (False, True):
+        c = make_cache([40], 2, 64, 64, 16, int8, poison=False)
+        binding.kv_append_paged(new[0], new[1], *_args(c), cu)
+        out, lse = binding.attn_decode_paged(q, *_args(c), 0.125, want_lse=True)
+        binding.last_device_status()
+        assert lse[0, :2].isfinite().all() and lse[0, 2:].isnan().all()
+        assert out[0, 2:].isnan().all() and out[0, :2, 60].isnan().all() and (int8 or out[0, :2, :60].isfinite().all())
+
+
 def test_append_reports_what_does_not_fit():
     c = make_cache([20, 20], 2, 64, 64, 16, seed=1, poison=False)
     new = torch.ones(4, 2, 64, dtype=torch.bfloat16, device="cuda")

@@ -420,7 +420,9 @@ typedef struct {
  * Puts new tokens into the cache.  seqlens: the lengths WITH the new tokens; sequence b has n_b = cu_new[b+1] - cu_new[b] of them
  * (0 <= n_b <= seqlens[b]), rows cu_new[b] ... of k_new / v_new, and row cu_new[b] + i goes to position seqlens[b] - n_b + i.
  *   k_new [n_rows, Hkv, D], v_new [n_rows, Hkv, Dv] BF16, 16-byte aligned, rows k_ld / v_ld elements apart (multiples of 8, so they may
- *   be slices of a projection's result); cu_new [B+1] INT32 (device), not falling; rows from cu_new[B] on (padding) are left out.
+ *   be slices of a projection's result); cu_new [B+1] INT32 (device), not falling, from 0 to n_rows; rows before cu_new[0] and from
+ *   cu_new[B] on (padding) are left out.  Other offsets are reported as bad lengths are, those of sequences without new tokens too; the results
+ *   are then unspecified.  With n_rows = 0 nothing is looked at.
  * BF16 caches: copied.  INT8 caches, per row: scale = max|x| / 127, code = clamp(rne(x / scale), -127, 127), in IEEE FP32 with
  * true divisions; a zero row gives scale 0 and codes 0, a row with a NaN scale NaN and codes 0, one with an infinity and no NaN scale
  * infinity and codes 0 (what is read back is then no number).

@@ -26,6 +26,7 @@ struct AppendParams {
   int64_t cap;
   int max_blocks, B;
   int heads, head_groups;       // KV heads a warp takes, groups of them
+  int row_ctas;                 // CTAs that take rows
   float* weights;
   int64_t ld;
   unsigned* status;
@@ -91,14 +92,32 @@ __device__ __noinline__ uint2 codes_by_division(uint4 v, float s) {
   return make_uint2(static_cast<uint32_t>(out), static_cast<uint32_t>(out >> 32));
 }
 
+// What no new row points at: lengths of sequences without new tokens, and offsets that fall or go past the rows that there are.  By CTAs of
+// their own behind those of the rows, so that it lengthens nobody's chain of loads.
+constexpr int kCheckedBy = 1024;            // sequences a CTA looks at
+__device__ __forceinline__ void check_sequences(const AppendParams& p, int cta) {
+  const int first = cta * kCheckedBy, last = min(p.B, first + kCheckedBy);
+  bool bad = false;
+  for (int b = first + static_cast<int>(threadIdx.x); b < last; b += kAppendThreads) {
+    const int32_t len = p.seqlens[b];
+    const int64_t begin = p.cu[b], end = p.cu[b + 1];
+    bad = bad || len < 0 || len > p.cap || begin < 0 || end < begin || end - begin > len || end > p.n_rows;
+  }
+  if (bad) atomicMax(p.status, kStatusBadShape);
+}
+
 constexpr int kAppendCtas = 7;              // resident on an SM at least
 template <bool kInt8, int kVecs>            // kVecs: 16-byte pieces of a BF16 row a lane holds (rows of up to 128 kVecs values)
 __global__ void __launch_bounds__(kAppendThreads, kAppendCtas)
 kv_append_kernel(const __grid_constant__ AppendParams p) {
   const int lane = threadIdx.x & 31, half = lane >> 4, hl = lane & 15;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * (kAppendThreads / 32);
+  const int64_t warps = static_cast<int64_t>(p.row_ctas) * (kAppendThreads / 32);
   pdl_wait_primary();
   pdl_launch_dependents();
+  if (static_cast<int>(blockIdx.x) >= p.row_ctas) {
+    check_sequences(p, blockIdx.x - p.row_ctas);
+    return;
+  }
   const int D = half ? p.c.Dv : p.c.D;
   const uint16_t* src = half ? p.v_new : p.k_new;
   const int64_t src_ld = half ? p.v_ld : p.k_ld;
@@ -178,10 +197,11 @@ kv_append_kernel(const __grid_constant__ AppendParams p) {
 }
 
 template <bool kInt8, int kVecs>
-msd_status_t launch_append(const AppendParams& p, cudaStream_t s) {
+msd_status_t launch_append(AppendParams& p, cudaStream_t s) {
   const int64_t per = kAppendThreads / 32, ctas = (p.n_rows * p.head_groups + per - 1) / per, most = 64LL * sm_count();
-  return launch_pdl(kv_append_kernel<kInt8, kVecs>, dim3(static_cast<unsigned>(ctas < most ? ctas : most)), dim3(kAppendThreads), 0, s,
-                    option(OPT_NO_PDL) != 1, p) == cudaSuccess
+  p.row_ctas = static_cast<int>(ctas < most ? ctas : most);
+  const int checkers = (p.B + kCheckedBy - 1) / kCheckedBy;
+  return launch_pdl(kv_append_kernel<kInt8, kVecs>, dim3(p.row_ctas + checkers), dim3(kAppendThreads), 0, s, option(OPT_NO_PDL) != 1, p) == cudaSuccess
              ? MSD_OK
              : (cudaGetLastError(), MSD_ERR_CUDA);
 }

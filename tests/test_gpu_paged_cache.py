@@ -538,6 +538,47 @@ def test_append_reports_what_does_not_fit():
     assert torch.equal(c["k"], before)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+def test_append_reports_lengths_and_rows_that_no_new_row_points_at(int8):
+    """Lengths of sequences without new tokens, more new tokens than rows, and offsets that fall are reported too; rows before the first
+    sequence and behind the last one are left out, and are no fault."""
+    c = make_cache([20, 20, 20], 2, 64, 64, 16, int8, seed=1, poison=False)
+    new = torch.ones(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    room = c["table"].shape[1] * 16
+
+    def append(lengths, cu, weights=None):
+        binding.kv_append_paged(new, new, c["k"], c["v"], c["k_scale"], c["v_scale"], c["table"], i32(*lengths), i32(*cu), weights=weights)
+        binding.last_device_status()
+
+    for lengths, cu in (((20, 20, 20), (0, 2, 2, 4)), ((20, 0, room), (0, 0, 0, 4)), ((20, 20, 20), (1, 2, 2, 3)), ((0, 0, 0), (0, 0, 0, 0))):
+        append(lengths, cu)
+    append((20, 20, 20), (0, 1, 1, 2), torch.zeros(3, 2, 20, device="cuda"))
+    for lengths, cu in (((20, -1, 20), (0, 2, 2, 4)), ((20, room + 1, 20), (0, 2, 2, 4)), ((2 ** 31 - 1, 20, 20), (0, 0, 0, 4)),
+                        ((20, 20, 20), (0, 2, 2, 5)), ((20, 20, 20), (0, 2, 1, 4)), ((20, 20, 20), (0, 4, 5, 4)), ((20, 20, 20), (-1, 2, 2, 4)),
+                        ((20, 20, 3), (0, 0, 0, 4)), ((-2, -2, -2), (0, 0, 0, 0))):
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            append(lengths, cu)
+    with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+        append((20, 21, 20), (0, 2, 2, 4), torch.zeros(3, 2, 20, device="cuda"))        # weights of fewer positions
+
+
+def test_append_looks_at_every_sequence_of_a_large_batch():
+    B = 5000
+    c = make_cache([4] * B, 1, 16, 16, 4, seed=1, poison=False)
+    new = torch.ones(3, 1, 16, dtype=torch.bfloat16, device="cuda")
+    cu = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    cu[1:] = 3
+    binding.kv_append_paged(new, new, *_args(c), cu)
+    binding.last_device_status()
+    for b in (0, 1, 127, 128, 1023, 1024, 4096, B - 1):
+        lengths = c["seqlens"].clone()
+        lengths[b] = -1
+        binding.kv_append_paged(new, new, c["k"], c["v"], None, None, c["table"], lengths, cu)
+        with pytest.raises(binding.MsdError, match="BAD_SHAPE"):
+            binding.last_device_status()
+
+
 # ---- eviction ----------------------------------------------------------------------------------------------------------------
 def _evict_case(lengths, Hkv, D, Dv, page, budget, int8, seed, layout="tokens"):
     """A cache with pages left for what is kept; the destination pages are in random order too."""

@@ -439,6 +439,8 @@ msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16,
  * query head h reading KV head h / (Hq / Hkv).  q and k are multiplied exactly (INT8 codes in FP16, q scaled by a power of two beside
  * them; the scales are applied in FP32) and summed in FP32; softmax in FP32; for the product with v, P is the sum of two BF16 values, with INT8
  * codes P times the value's scale is one FP16 value: 11 bits down to 2^-21 of the largest scale so far, off by 2^-32 of that below.
+ * No sum overflows over finite values (value scales up to 2^127), and an infinite BF16 value comes out as one for every token
+ * whose probability is above 2^-60 of the largest (below, it may give NaN).
  * No decomposition: this is the cache read as it is, beside msd_attn_decode_int8kv_paged, which splits q and P into INT8 components.
  *   q_bf16 [B, Hq, D], rows of a sequence q_ld elements apart (a multiple of 8); out_bf16 [B, Hq, Dv]; lse nullable [B, Hq] FP32
  *   (natural-log sum of exp of the scaled scores).  Hq % Hkv == 0.  Empty sequences give zeros and lse = -inf.

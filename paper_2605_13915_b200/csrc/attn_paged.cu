@@ -20,7 +20,7 @@
 //
 // Precision: q and k (codes) are multiplied exactly and summed in FP32; the sums' error is what an FP32 product has.  P for the
 // product with v is two BF16 values, or one FP16 value with 11 bits for codes; one BF16 value made the result's error 1.4 times that of
-// its own rounding to BF16.
+// its own rounding to BF16.  Of the two, both are above 0 where P is, or an infinite value times them would be no number.
 //
 // Split over the length: the tiles of all sequences form one list, cut into equal runs; run i is walked by U = KV heads x head groups
 // CTAs side by side, one per unit, so that CTAs that run together read neighbouring rows.  The grid is what is resident at once.
@@ -48,6 +48,9 @@ constexpr int kAtOnceWeights = 4;           // positions of a thread whose score
 constexpr int kClusterTiles = 4, kClusterCtas = 16;     // one kernel: most tiles of a CTA, most CTAs of a unit
 constexpr float kHeld = 8.0f;               // how far (log2) a score may exceed its reference before that moves
 constexpr float kPUnits = 128.0f;           // INT8: 2^15 / 2^kHeld
+// Sums of P and of P v are kept times kDown, so that the sum over 2^31 tokens of P <= 2^kHeld is less than 1 and no sum of finite values
+// overflows.  (A power of two: nothing rounds elsewhere.)
+constexpr float kDown = 1.8189894035458565e-12f, kUp = 1.0f / kDown;      // 2^-39
 
 struct PagedAttnParams {
   PagedCache c;
@@ -67,8 +70,8 @@ struct PagedAttnParams {
   int score_heads;            // heads of a position's scores: G, made even
   int slots;                  // head slots of a CTA, 8, 16 or 24
   // workspace
-  float* part;                // [CTA][2][rows][Dv]: unnormalised outputs
-  float* part_ml;             // [CTA][2][rows][2]: maximum (log2) and sum
+  float* part;                // [CTA][2][rows][Dv]: unnormalised outputs, times kDown
+  float* part_ml;             // [CTA][2][rows][2]: maximum (log2), and sum times kDown
   int4* tail;                 // [CTA] {sequence cut at the end of its run or -1, first and last run of that sequence}
   int2* seq_runs;             // [B] {first, last run}
   float* lse2;                // [B, Hq] log2-sum of uncut sequences' scores
@@ -118,6 +121,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+__device__ __forceinline__ uint32_t high_halves(float lo, float hi) {      // BF16 values, cut off
+  return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
@@ -273,7 +279,7 @@ __device__ __forceinline__ void join_tail(const PagedAttnParams& p, int tid, int
       }
       const float inv = 1.0f / l;
       *reinterpret_cast<uint2*>(p.out + (out0 + r) * Dv + d) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-      if (d == 0 && p.lse) p.lse[out0 + r] = (m + log2f(l)) * 0.6931471805599453f;
+      if (d == 0 && p.lse) p.lse[out0 + r] = (m + log2f(l * kUp)) * 0.6931471805599453f;
     }
   }
 }
@@ -319,7 +325,7 @@ __device__ __forceinline__ void add_weights(const PagedAttnParams& p, int tid, i
       const float om = __shfl_xor_sync(0xffffffffu, m, d), ol = __shfl_xor_sync(0xffffffffu, l, d);
       join_pair(m, l, om, ol);
     }
-    return m + log2f(l);
+    return m + log2f(l * kUp);
   };
   if constexpr (kThreads == 32) {                // four lanes a head
     const float lg = lse2(min(tid >> 2, p.G - 1), tid & 3, 4);
@@ -868,7 +874,8 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         }
       }
       // Probabilities as column fragments of the product with v: the transposes of the score fragments.  INT8: times the value's scale,
-      // in FP16 (11 bits).  BF16: the 8 bits of one BF16 would double the error of the result, so what they leave out goes in too.
+      // in FP16 (11 bits).  BF16: the 8 bits of one BF16 would double the error of the result, so what they leave out goes in too.  They are
+      // cut off, not rounded, and the last bit of P is set, so that what is left out is above 0: at most 2^-7 of P, rounded to 8 bits (2^-16).
       uint2 ph[kGroups][NT], pl[kGroups][NT];
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
@@ -879,12 +886,13 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
           for (int e = 0; e < 4; ++e) {
             const float mm = m[n][e & 1];
             x[e] = ex2(s[g][n][e] - (mm == -INFINITY ? 0.0f : mm));
+            if constexpr (!kInt8) x[e] = __uint_as_float(__float_as_uint(x[e] * kDown) | 1u);
             l[n][e & 1] += x[e];
           }
           if constexpr (kInt8) {
             ph[g][n] = make_uint2(transposed(pack_f16(x[0] * vs[g][0], x[1] * vs[g][0])), transposed(pack_f16(x[2] * vs[g][1], x[3] * vs[g][1])));
           } else {
-            const uint32_t a = pack_bf16(x[0], x[1]), c = pack_bf16(x[2], x[3]);
+            const uint32_t a = high_halves(x[0], x[1]), c = high_halves(x[2], x[3]);
             ph[g][n] = make_uint2(transposed(a), transposed(c));
             pl[g][n] = make_uint2(transposed(pack_bf16(x[0] - __uint_as_float(a << 16), x[1] - __uint_as_float(a & 0xFFFF0000u))),
                                   transposed(pack_bf16(x[2] - __uint_as_float(c << 16), x[3] - __uint_as_float(c & 0xFFFF0000u))));
@@ -937,7 +945,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
         if (row == 0) {
           const int h = n * 8 + 2 * quad + e;
           ml[0][warp][h] = m[n][e];
-          ml[1][warp][h] = l[n][e];
+          ml[1][warp][h] = kInt8 ? l[n][e] * kDown : l[n][e];
           if constexpr (kInt8) ml[2][warp][h] = vref * (1.0f / kPUnits);
         }
       }
@@ -957,7 +965,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
               if constexpr (kInt8) {
-                *reinterpret_cast<float2*>(dst + i * 16 + 2 * row) = make_float2(o[n][i][e], o[n][i][2 + e]);
+                *reinterpret_cast<float2*>(dst + i * 16 + 2 * row) = make_float2(o[n][i][e] * kDown, o[n][i][2 + e] * kDown);
               } else {
                 dst[i * 16 + row] = o[n][i][e];
                 dst[i * 16 + row + 8] = o[n][i][2 + e];
@@ -993,7 +1001,7 @@ attn_paged_kernel(const __grid_constant__ PagedAttnParams p) {
           const int64_t out_row = static_cast<int64_t>(b) * p.Hq + head0 + h;
           *reinterpret_cast<uint2*>(p.out + out_row * Dv + d) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
           if (d == 0) {
-            const float lg = mh + log2f(lh);
+            const float lg = mh + log2f(lh * kUp);
             if (p.lse) p.lse[out_row] = lg * 0.6931471805599453f;
             if (p.weights) p.lse2[out_row] = lg;
           }

@@ -250,6 +250,49 @@ def test_attention_passes_nan_on(length, first, last, int8):
     assert torch.equal(weights[1][1], weights[0][1])
 
 
+@pytest.mark.parametrize("lengths,Hq,Hkv,D", [([1, 33], 4, 2, 64), ([200], 32, 8, 128), ([9000, 700], 16, 4, 128), ([40000], 20, 1, 64), ([450], 40, 2, 192),
+                                              ([3000], 2, 2, 256)])
+def test_attention_of_infinite_values(lengths, Hq, Hkv, D):
+    """An infinity among the values of a token comes out as one, whatever the bits of the token's probability are: of every head that reads
+    it, and the rest of the results is what it was.  (Probabilities are above 2^-40 here.)"""
+    c = make_cache(lengths, Hkv, D, D, 16, seed=33)
+    g = torch.Generator().manual_seed(33)
+    q = torch.randn(len(lengths), Hq, D, generator=g).to(torch.bfloat16).cuda()
+    want, want_lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, want_lse=True)
+    G = Hq // Hkv
+    there = torch.zeros(want.shape, device="cuda")
+    for b, n in enumerate(lengths):
+        for d in range(1, D - 1):
+            j, h, sign = int(torch.randint(n, (1,), generator=g)), d % Hkv, 1 - 2 * (d // Hkv % 2)
+            c["v"][c["table"][b, j // 16], j % 16, h, d] = sign * float("inf")
+            there[b, h * G:(h + 1) * G, d] = sign
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, want_lse=True)
+    binding.last_device_status()
+    assert torch.equal(out, torch.where(there == 0, want, (there * float("inf")).to(torch.bfloat16))) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("factor", [1e38, -1e38, 1e-24])
+@pytest.mark.parametrize("lengths,Hq,Hkv,D", [([1, 33], 4, 2, 64), ([200], 32, 8, 128), ([9000, 700], 16, 4, 128), ([40000], 20, 1, 64), ([3000], 2, 2, 256)])
+def test_attention_of_values_at_the_ends_of_their_range(lengths, Hq, Hkv, D, factor, int8):
+    """Values of 1e38 to 3e38, whose sum over the tokens no FP32 number holds, and of 1e-24: their mean is a number of that size."""
+    c = make_cache(lengths, Hkv, D, D, 16, int8, seed=34, poison=False)
+    g = torch.Generator().manual_seed(34)
+    if int8:
+        c["v"].copy_(torch.randint(1, 128, c["v"].shape, generator=g))
+        c["v_scale"].copy_((torch.rand(c["v_scale"].shape, generator=g) + 1.25) * abs(factor) / 127)
+        if factor < 0:
+            c["v"].neg_()
+    else:
+        c["v"].copy_(((torch.rand(c["v"].shape, generator=g) * 2 + 1) * factor).to(torch.bfloat16))
+    q = torch.randn(len(lengths), Hq, D, generator=g).to(torch.bfloat16).cuda()
+    before = torch.zeros(len(lengths), Hkv, max(lengths), device="cuda")
+    weights = before.clone()
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+
+
 def test_attention_with_unequal_scales():
     """Values whose scales are a million times apart.  P times the scale is FP16 in units of the largest scale: below 2^-21 of it the
     error is 2^-32 of that scale (rounded up to a power of two) for each token, times its code."""

@@ -72,7 +72,7 @@ msd_status_t msd_debug_timeout_selftest(int64_t budget_cycles, void* stream);
  *   calls on the tile kernel, else 100000 x K blocks per stage + 1000 x CTAs per band + weight rows per band),
  *   MSD_ATTN_SPLITS / MSD_ATTN_CHUNK_TILES (context splits of the attention kernels; msd_attn_decode_schedule reports the schedule in force),
  *   MSD_ATTN_BALANCED (1: the balanced split schedule for every shape that has a kernel for it, 0: never; a forced
- *   split count or size switches it off as well). */
+ *   split count or size switches it off as well), MSD_ATTN_CLUSTER (0: the paged attention as if its clusters could not be launched). */
 msd_status_t msd_debug_set_option(const char* name, int32_t value);
 void msd_debug_reset_options(void);
 

@@ -1108,7 +1108,8 @@ template <bool kInt8, int DP, int kHeads>
 msd_status_t launch_paged(const PagedAttnParams& p, bool cluster, cudaStream_t s) {
   const bool pdl = option(OPT_NO_PDL) != 1;
   if constexpr (kHeads == 8) {
-    if (cluster) return launch_runs<kInt8, DP, kHeads, true>(p, s, pdl) ? MSD_OK : MSD_ERR_CUDA;
+    // (clusters of more than 8 CTAs are not promised by every device or part of one: without them two kernels do, with as many runs)
+    if (cluster && option(OPT_ATTN_CLUSTER) != 0 && launch_runs<kInt8, DP, kHeads, true>(p, s, pdl)) return MSD_OK;
   }
   if (!launch_runs<kInt8, DP, kHeads, false>(p, s, pdl)) return MSD_ERR_CUDA;
   if (p.runs == 1 && !p.weights) return MSD_OK;      // (every sequence was finished by one CTA)

@@ -31,6 +31,7 @@ enum Option {
   OPT_ATTN_SPLITS,          // MSD_ATTN_SPLITS: number of context splits of the attention kernels
   OPT_ATTN_CHUNK_TILES,     // MSD_ATTN_CHUNK_TILES: tiles per context split
   OPT_ATTN_BALANCED,        // MSD_ATTN_BALANCED: 1 balanced schedule wherever a kernel for it exists, 0 never
+  OPT_ATTN_CLUSTER,         // MSD_ATTN_CLUSTER: 0 as if the one-kernel form of the paged attention could not be launched
   OPT_COUNT
 };
 int option(Option o);

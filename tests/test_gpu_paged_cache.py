@@ -168,6 +168,22 @@ def test_attention_over_few_tiles(lengths, Hq, Hkv, D, Dv, int8):
     assert torch.equal(binding.attn_decode_paged(q, *_args(c), D ** -0.5), got[0][0])
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("lengths,Hq,Hkv,D,Dv", FEW)
+def test_attention_over_few_tiles_where_a_cluster_is_refused(lengths, Hq, Hkv, D, Dv, int8):
+    """The call goes on with two kernels, in the same workspace."""
+    B, ld = len(lengths), max(max(lengths), 1)
+    c = make_cache(lengths, Hkv, D, Dv, 16, int8, seed=sum(lengths))
+    q = torch.randn(B, Hq, D, generator=torch.Generator().manual_seed(D)).to(torch.bfloat16).cuda()
+    before = torch.rand(B, Hkv, ld, generator=torch.Generator().manual_seed(B)).cuda()
+    weights = before.clone()
+    binding.debug_set_option("MSD_ATTN_CLUSTER", 0)
+    out, lse = binding.attn_decode_paged(q, *_args(c), D ** -0.5, weights=weights, want_lse=True)
+    binding.last_device_status()
+    _check_attention(q, c, D ** -0.5, out, lse, before, weights)
+    assert torch.equal(binding.attn_decode_paged(q, *_args(c), D ** -0.5), out)
+
+
 def test_attention_with_more_heads_than_places_on_the_machine():
     """Every CTA walks all sequences of its KV head; one query head each, and 8 groups of 16 for the others."""
     for Hq, Hkv in ((900, 900), (640, 5)):

@@ -446,6 +446,7 @@ msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16,
  *   (natural-log sum of exp of the scaled scores).  Hq % Hkv == 0.  Empty sequences give zeros and lse = -inf.
  *   weights nullable [B, Hkv, ld] FP32: weights[b][k][j] += the sum of P_hj over the heads h of KV head k, for j < seqlens[b]; the
  *   rest is left as it is.  ld >= every length.  The sums have a fixed order: equal inputs give equal bits.
+ * out_bf16 lies over no row of q (MSD_ERR_UNSUPPORTED): one that is done may be written while others still read theirs.
  * workspace: >= msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld) bytes (ld = 0 without weights; with them it holds a score of every
  * head and position, about 4 B Hq ld bytes), 1024-byte aligned, no initialisation needed.  One kernel or two; nothing is kept from call to call.  The rows of k and of v may spread over 64 GiB each, the scales
  * over 16 GiB, and B sequences as long as the table has room for may come to 2^36 tokens (more: MSD_ERR_UNSUPPORTED).
@@ -465,8 +466,8 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
  * The rows (and INT8 scales) are COPIED to the pages of dst_block_table [B, dst_max_blocks], which has room for min(L, budget) tokens
  * of each sequence; the old pages are only read, so they may be shared with sequences outside the call, and are the caller's
  * to hand out again afterwards.  A page of dst_block_table appears nowhere else in it and in no row of block_table; the same pointer
- * for both is MSD_ERR_UNSUPPORTED, and so are new_weights == weights and new_seqlens == seqlens.  The rows of k and of v may spread over
- * 64 GiB each (more: MSD_ERR_UNSUPPORTED).
+ * for both is MSD_ERR_UNSUPPORTED, and so are new_seqlens, new_weights or kept that lie over one another or over what the call reads.  The
+ * rows of k and of v may spread over 64 GiB each (more: MSD_ERR_UNSUPPORTED).
  */
 msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* block_table, int32_t max_blocks, const int32_t* seqlens,
                                 const float* weights, int64_t ld, int32_t B, int32_t budget, int32_t recent, int32_t sinks,

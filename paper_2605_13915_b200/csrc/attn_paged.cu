@@ -1188,6 +1188,12 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
       !aligned(seqlens, 4) || !aligned(lse, 4) || !aligned(weights, 4))
     return MSD_ERR_BAD_ALIGNMENT;
   if (workspace_bytes < pl.bytes) return MSD_ERR_WORKSPACE_TOO_SMALL;
+  // A query is read by all runs of its sequence and KV head; the first to end may write.  Rows of q that end behind the start of `out`
+  // and begin before its end:
+  const int64_t q_row = static_cast<int64_t>(Hq) * cache->D * 2, out_bytes = static_cast<int64_t>(B) * Hq * cache->Dv * 2;
+  const __int128 q_end = static_cast<__int128>(reinterpret_cast<uintptr_t>(out_bf16)) - reinterpret_cast<uintptr_t>(q_bf16) - q_row, step = static_cast<__int128>(q_ld) * 2;
+  const __int128 row = q_end < 0 ? 0 : q_end / step + 1;       // the first that ends behind the start of `out`
+  if (row < B && row * step < q_end + q_row + out_bytes) return MSD_ERR_UNSUPPORTED;
   const int64_t page = cache->page_size, blocks = cache->num_blocks, most_rows = int64_t{1} << 36, most_scales = int64_t{1} << 34;
   if (!rows_within(p.c.k, blocks, page, most_rows) || !rows_within(p.c.v, blocks, page, most_rows) ||
       (int8 && !(rows_within(p.c.ks, blocks, page, most_scales) && rows_within(p.c.vs, blocks, page, most_scales))))

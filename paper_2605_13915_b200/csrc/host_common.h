@@ -68,6 +68,11 @@ class DeviceOnce {
 };
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// Whether [a, a + a_bytes) and [b, b + b_bytes) have a byte in common.
+inline bool overlap(const void* a, __int128 a_bytes, const void* b, __int128 b_bytes) {
+  const __int128 a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  return a0 < b0 + b_bytes && b0 < a0 + a_bytes;
+}
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // attn_decode.cu: merges the context splits' partial results [rows][n_splits][4 + Dv] into out_bf16 [rows][Dv] (and lse)

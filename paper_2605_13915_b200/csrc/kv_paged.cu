@@ -637,10 +637,20 @@ msd_status_t msd_kv_evict_paged(const msd_paged_cache_t* cache, const int32_t* b
   if (!block_table || !seqlens || !weights || !dst_block_table || !new_seqlens || !new_weights || !kept) return MSD_ERR_NULL_POINTER;
   if (!rows_within(p.c.k, cache->num_blocks, cache->page_size, int64_t{1} << 36) || !rows_within(p.c.v, cache->num_blocks, cache->page_size, int64_t{1} << 36))
     return MSD_ERR_UNSUPPORTED;
-  if (block_table == dst_block_table || weights == new_weights || seqlens == new_seqlens) return MSD_ERR_UNSUPPORTED;
+  if (block_table == dst_block_table) return MSD_ERR_UNSUPPORTED;
   if (!aligned(block_table, 4) || !aligned(seqlens, 4) || !aligned(weights, 4) || !aligned(dst_block_table, 4) || !aligned(new_seqlens, 4) ||
       !aligned(new_weights, 4) || !aligned(kept, 4))
     return MSD_ERR_BAD_ALIGNMENT;
+  // what is written lies in nothing that is read, and nothing is written twice
+  const __int128 heads = static_cast<__int128>(B) * cache->Hkv;
+  const struct { const void* at; __int128 bytes; } written[] = {{new_seqlens, B * 4LL}, {new_weights, heads * new_ld * 4}, {kept, heads * budget * 4}},
+      read[] = {{block_table, B * 4LL * max_blocks}, {dst_block_table, B * 4LL * dst_max_blocks}, {seqlens, B * 4LL}, {weights, heads * ld * 4}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& r : read)
+      if (overlap(written[i].at, written[i].bytes, r.at, r.bytes)) return MSD_ERR_UNSUPPORTED;
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[i].at, written[i].bytes, written[j].at, written[j].bytes)) return MSD_ERR_UNSUPPORTED;
+  }
   p.status = device_status_ptr();
   if (!p.status) return MSD_ERR_CUDA;
   p.table = block_table;

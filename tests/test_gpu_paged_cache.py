@@ -788,6 +788,37 @@ def test_wrappers_refuse_tensors_that_do_not_fit():
     binding.last_device_status()
 
 
+def test_results_in_the_place_of_inputs_are_refused():
+    """Attention whose results would overwrite queries that other CTAs still read, and an eviction that writes into what it reads; buffers
+    that only touch are taken."""
+    c = make_cache([5000, 40], 2, 64, 64, 16, seed=35, poison=False)
+    g = torch.Generator().manual_seed(35)
+    q = torch.randn(2, 8, 64, generator=g).to(torch.bfloat16).cuda()
+    want = binding.attn_decode_paged(q, *_args(c), 0.125)
+    room = torch.zeros(4 * 8 * 64 + 8, dtype=torch.bfloat16, device="cuda")
+    room[:1024] = q.flatten()
+    at = lambda first: room[first:first + 1024].view(2, 8, 64)
+    for first in (0, 8, 1016):
+        with pytest.raises(binding.MsdError, match="UNSUPPORTED"):
+            binding.attn_decode_paged(at(0), *_args(c), 0.125, out=at(first))
+    assert torch.equal(binding.attn_decode_paged(at(0), *_args(c), 0.125, out=at(1024)), want)
+    # between the rows of a slice
+    wide = torch.zeros(2, 2048, dtype=torch.bfloat16, device="cuda")
+    wide[:, :512] = q.flatten(1)
+    rows = wide[:, :512].unflatten(1, (8, 64))
+    assert torch.equal(binding.attn_decode_paged(rows, *_args(c), 0.125, out=wide[0, 512:1536].view(2, 8, 64)), want)
+    with pytest.raises(binding.MsdError, match="UNSUPPORTED"):
+        binding.attn_decode_paged(rows, *_args(c), 0.125, out=wide.flatten()[1032:2056].view(2, 8, 64))
+    dst = torch.arange(2, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    arena = torch.zeros(100000, device="cuda")
+    w = arena[:2 * 2 * 5000].view(2, 2, 5000)
+    for changes in ({"new_weights": arena[19999:19999 + 64].view(2, 2, 16)}, {"new_weights": arena[:64].view(2, 2, 16)},
+                    {"kept": arena[19990:19990 + 64].view(torch.int32).view(2, 2, 16)}, {"new_seqlens": c["seqlens"]}, {"new_seqlens": dst.flatten()}):
+        with pytest.raises(binding.MsdError, match="UNSUPPORTED"):
+            binding.kv_evict_paged(*_args(c), w, 16, dst, **changes)
+    binding.last_device_status()
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("int8", [False, True])
 def test_decoding_loop(int8):

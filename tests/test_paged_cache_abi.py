@@ -107,6 +107,24 @@ def test_eviction_refuses():
     assert _evict(c, weights=P + 2) == ALIGN and _evict(c, kept=P + 2) == ALIGN
 
 
+def test_results_over_inputs_are_refused():
+    """Each range that a call writes against each that it reads, from the first common byte to the last."""
+    c = _cache()
+    row, out = 4 * 64 * 2, 2 * 4 * 64 * 2                                       # bytes of a query row and of the results of two sequences
+    far = 1 << 20
+    for at in (P, P + 16, P + row - 16, P - out + 16, P + far, P + far + row - 16, P + far - out + 16, P + far - row):
+        assert _attend(c, q=P, q_ld=far // 2, out=at, ws=far * far) == UNSUPPORTED, at
+    base = dict(table=1 << 20, seqlens=2 << 20, weights=3 << 20, dst=4 << 20, new_seqlens=5 << 20, new_weights=6 << 20, kept=7 << 20)
+    size = dict(table=2 * 4 * 4, seqlens=8, weights=2 * 2 * 64 * 4, dst=2 * 2 * 4, new_seqlens=8, new_weights=2 * 2 * 32 * 4, kept=2 * 2 * 32 * 4)
+    written = ("new_seqlens", "new_weights", "kept")
+    for w in written:
+        for r in size:
+            if r == w:
+                continue
+            for at in (base[r], base[r] + size[r] - 4, base[r] - size[w] + 4):
+                assert _evict(c, **dict(base, **{w: at})) == UNSUPPORTED, (w, r, at)
+
+
 def test_call_module_takes_cuda_tensors_only():
     calls = binding._calls()
     t = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype)

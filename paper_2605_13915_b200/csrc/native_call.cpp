@@ -359,7 +359,7 @@ PyObject* kv_append_paged(PyObject* const* args, Py_ssize_t n) {
              "k_new and v_new do not fit the cache") ||
       !agree(a, table->size(0) == len->size(0) && cu->size(0) == len->size(0) + 1, "block_table, seqlens and cu_new differ in their sequences") ||
       !agree(a, len->size(0) <= 0x7FFFFFFF && table->size(1) <= 0x7FFFFFFF, "a size is too large") ||
-      !agree(a, !w || (w->size(0) == len->size(0) && w->size(1) == c.Hkv), "weights: [sequences, KV heads, positions]"))
+      !agree(a, !w || (w->size(0) == len->size(0) && w->size(1) == c.Hkv && w->size(2) > 0), "weights: [sequences, KV heads, positions]"))
     return nullptr;
   void *knp = addr(kn), *vnp = addr(vn), *st = stream();
   const int64_t rows = kn->size(0), k_ld = row_stride(kn), v_ld = row_stride(vn), ld = w ? w->size(2) : 0;
@@ -385,7 +385,7 @@ PyObject* attn_decode_paged(PyObject* const* args, Py_ssize_t n) {
       !agree(a, q->size(0) <= 0x7FFFFFFF && q->size(1) <= 0x7FFFFFFF && table->size(1) <= 0x7FFFFFFF, "a size is too large") ||
       !agree(a, out->size(0) == q->size(0) && out->size(1) == q->size(1) && out->size(2) == c.Dv, "out: [sequences, heads, size of a value]") ||
       !agree(a, !lse || (lse->size(0) == q->size(0) && lse->size(1) == q->size(1)), "lse: [sequences, heads]") ||
-      !agree(a, !w || (w->size(0) == q->size(0) && w->size(1) == c.Hkv), "weights: [sequences, KV heads, positions]"))
+      !agree(a, !w || (w->size(0) == q->size(0) && w->size(1) == c.Hkv && w->size(2) > 0), "weights: [sequences, KV heads, positions]"))
     return nullptr;
   const Workspace room(ws);
   void *qp = addr(q), *op = addr(out), *st = stream();

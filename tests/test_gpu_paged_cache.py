@@ -819,6 +819,15 @@ def test_results_in_the_place_of_inputs_are_refused():
     binding.last_device_status()
 
 
+def test_weights_without_a_position_are_refused():
+    c = make_cache([5], 2, 64, 64, 16, poison=False)
+    q, none = torch.ones(1, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 2, 0, device="cuda")
+    with pytest.raises(ValueError):
+        binding.attn_decode_paged(q, *_args(c), 0.1, weights=none)
+    with pytest.raises(ValueError):
+        binding.kv_append_paged(q[:, :2], q[:, :2], *_args(c), torch.tensor([0, 1], dtype=torch.int32, device="cuda"), weights=none)
+
+
 # ---- together ------------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("int8", [False, True])
 def test_decoding_loop(int8):

@@ -1,11 +1,13 @@
 """The paged cache on the GPU: appending, attention of one new token with the weights of the cached tokens, eviction; each against
 plain 64-bit loops, at the sizes and masks where it can go wrong, and all of them as a decoding loop runs them."""
+import os
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2605_13915_b200 import binding, inputs
-from paged_reference import attention, evicted, make_cache
+from paged_reference import attention, evicted, make_cache, sequence
 
 pytestmark = pytest.mark.gpu
 
@@ -906,6 +908,50 @@ def test_decoding_loop(int8):
             for pool in (k, v):
                 pool[tables[1 - at].flatten().long()] = 127 if int8 else float("nan")
     binding.last_device_status()
+
+
+def test_the_loop_of_the_readme_goes_on_after_an_eviction():
+    """README's lines, run as they stand for three steps, an eviction in each: the attention reads the tokens that were kept, on the pages
+    they went to, and the new one."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        text = f.read().split("### A decoding loop around a paged cache")[1].split("\n## ")[0]
+    lines = "\n".join(line[4:] for line in text.splitlines() if line.startswith("    "))
+    Hkv, D, page, width, B, budget = 2, 64, 16, 20, 2, 280
+    g = torch.Generator().manual_seed(36)
+    c = make_cache([300, 290], Hkv, D, D, page, int8=True, seed=36, poison=False, spare=2 * B * width)
+    used = set(c["table"][c["table"] >= 0].tolist())
+    free = torch.tensor([x for x in range(c["k"].shape[0]) if x not in used], dtype=torch.int32)
+    tables = [torch.full((B, width), -1, dtype=torch.int32, device="cuda"), free[:B * width].view(B, width).cuda()]
+    tables[0][:, :c["table"].shape[1]] = c["table"]
+    names = {"k": c["k"], "v": c["v"], "ks": c["k_scale"], "vs": c["v_scale"], "block_table": tables[0], "seqlens": c["seqlens"],
+             "weights": torch.rand(B, Hkv, page * width, generator=g).cuda(), "cu_new": torch.arange(B + 1, dtype=torch.int32, device="cuda"),
+             "scale": 0.125, "budget": budget, "ws": binding.workspace(binding.attn_decode_paged_workspace_bytes(B, 8, Hkv, D, page * width))}
+    held = {x: [[list(sequence(c, b, x)[:, h].cpu()) for h in range(Hkv)] for b in range(B)] for x in ("k", "v")}      # rows of each head, in order
+    spare = free[B * width:2 * B * width].view(B, width).cuda()
+    for step in range(3):
+        names["seqlens"] = names["seqlens"] + 1
+        names["new_block_table"] = (tables[1], spare)[step % 2]
+        for x in ("k", "v"):
+            new = torch.randn(B, Hkv, D, generator=g).to(torch.bfloat16)
+            names[x + "_new"] = new.cuda()
+            codes, s = inputs.quantize_rows_int8(new.view(torch.int16).numpy().view(np.uint16))
+            rows = torch.from_numpy(codes).double() * torch.from_numpy(np.asarray(s)).double()[..., None]
+            for b in range(B):
+                for h in range(Hkv):
+                    held[x][b][h].append(rows[b, h])
+        names["q"] = torch.randn(B, 8, D, generator=g).to(torch.bfloat16).cuda()
+        exec(lines, names)
+        binding.last_device_status()
+        for b in range(B):
+            for h in range(Hkv):
+                K, V = torch.stack(held["k"][b][h]), torch.stack(held["v"][b][h])
+                p = torch.softmax(names["q"][b, 4 * h:4 * h + 4].double().cpu() @ K.T * 0.125, -1)
+                # two roundings to 8 bits or more, and the FP32 part, which stays below 2^-12 here
+                bound = HALF_BF16 * (p @ V).abs() + (HALF_BF16 + 2.0 ** -12) * (p @ V.abs())
+                assert ((names["out"][b, 4 * h:4 * h + 4].double().cpu() - p @ V).abs() <= bound).all(), step
+                for x in ("k", "v"):
+                    held[x][b][h] = [held[x][b][h][j] for j in names["kept"][b, h].tolist()]
+        assert names["seqlens"].tolist() == [budget, budget]
 
 
 @pytest.mark.parametrize("int8", [False, True])

@@ -448,7 +448,7 @@ msd_status_t msd_kv_append_paged(const void* k_new_bf16, const void* v_new_bf16,
  *   rest is left as it is.  ld >= every length.  The sums have a fixed order: equal inputs give equal bits.
  * out_bf16 lies over no row of q (MSD_ERR_UNSUPPORTED): one that is done may be written while others still read theirs.
  * workspace: >= msd_attn_decode_paged_workspace_bytes(B, Hq, Hkv, Dv, ld) bytes (ld = 0 without weights; with them it holds a score of every
- * head and position, about 4 B Hq ld bytes), 1024-byte aligned, no initialisation needed.  One kernel or two; nothing is kept from call to call.  The rows of k and of v may spread over 64 GiB each, the scales
+ * head and position: 4 B Hkv ld bytes times the heads of a KV head, rounded up to an even number), 1024-byte aligned, no initialisation needed.  One kernel or two; nothing is kept from call to call.  The rows of k and of v may spread over 64 GiB each, the scales
  * over 16 GiB, and B sequences as long as the table has room for may come to 2^36 tokens (more: MSD_ERR_UNSUPPORTED).
  */
 size_t msd_attn_decode_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t Dv, int64_t ld);

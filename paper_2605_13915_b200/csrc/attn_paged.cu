@@ -4,7 +4,7 @@
 //   S_hj = scale q_h.k_j,  P = softmax(S),  out = P V,  weights_j += sum_h P_hj
 //
 // Bound: HBM.  A token of a KV head is 2 (D + Dv) bytes (BF16) for 2 G (D + Dv) multiply-adds of its G query heads.  An SM takes in
-// 44 bytes a nanosecond, 23 a clock, and the warp-level MMAs of that (8 or 16 head slots, used or not) are a fifth of what the pipe does,
+// 44 bytes a nanosecond, 23 a clock, and the warp-level MMAs of that (8, 16 or 24 head slots, used or not) are a fifth of what the pipe does,
 // so nothing here waits for the tensor cores, and what counts is that loads never stop.  Hence no roles and no hand-offs: each warp
 // keeps a ring of token tiles of its own in flight (cp.async, a row's page looked up a tile ahead), multiplies a tile against the
 // query fragments in its registers, keeps its own references, sums and outputs, and meets the other warps of its CTA only when
@@ -145,7 +145,8 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t u) {
 }
 
 // DP: D and Dv rounded up to 64, 96, 128, 192 or 256; kHeads: head slots of a CTA, 8, 16 or 24.  A tile of a warp is 16 or 32 tokens, 4 to 16 KB
-// of keys and values; the rings of an SM's CTAs hold 140 to 200 KB.  Two stages and as many warps as their registers allow (heads of 128, 32 x
+// of keys and values; the rings of an SM's CTAs hold 144 to 192 KB (BF16), and 130 to 198 KB (INT8), less where registers allow two or three CTAs of small
+// tiles: INT8 rows of 64 102 KB with 16 slots and 68 with 24, of 96 100 with 24.  Two stages and as many warps as their registers allow (heads of 128, 32 x
 // 2048-8192 tokens: INT8 81 / 85 us, 16 / 16 heads of 80 52 / 57 with more stages and fewer warps; at the same number of warps a third
 // stage, 24 x 1024-4096: 16 / 16 heads of 64 INT8 39.9 / 44.0, of 256 99 / 101), but for BF16 with two CTAs an SM (128 / 8 heads of 128: 53.5 with two
 // stages, 52.6 with three).  Sizes of 96 and 192 beside the powers of two: 128 / 8 heads of 80 BF16 48 -> 42 us, INT8 45 -> 39, 16 / 16 heads
@@ -1222,7 +1223,8 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   p.seqlens = seqlens;
   p.max_blocks = max_blocks;
   // Keys and values that L2 can hold a part of until the next step leave it before anything else does, or a part of them is never there
-  // when it is asked for again: 64/8 heads, 24 x 512-4096 tokens INT8 34.3 / 32.4 us without / with, 16/16 heads of 80, 48 x 0-1500 51 / 47;
+  // when it is asked for again.  (Measured on caches that the next call reads again; between a model's layers little of one is left, and either will do.)
+  // 64/8 heads, 24 x 512-4096 tokens INT8 34.3 / 32.4 us without / with, 16/16 heads of 80, 48 x 0-1500 51 / 47;
   // of more than that nothing stays either way, and it costs 3 % (2 x 100000-131072 BF16 164 / 169 us).
   p.leave_l2 = static_cast<double>(p.cap) * B * cache->Hkv * (cache->D + cache->Dv) * (int8 ? 1 : 2) <= 512e6;
   p.B = B;
@@ -1236,6 +1238,7 @@ msd_status_t msd_attn_decode_paged(const void* q_bf16, int64_t q_ld, const msd_p
   // runs; so a CTA has no more tiles than in the other form, or up to four of a single sequence (a second sequence costs more than a second
   // tile).  32/8 heads of 128 on the GPU, two kernels / one: BF16 1 x 1000 tokens 8.0 / 6.9 us, 1 x 4000 13.1 / 9.7, 4 x 128-256 with weights 7.8 /
   // 7.1, INT8 1 x 4000 with weights 11.9 / 10.4, 8 x 128-256 9.3 / 8.4; 16 x 32-64 with weights 6.9 / 7.5.  The call's host time goes from 6.4 to 4.2 us.
+  // (`room` is the table's: with a table for more tokens, short sequences are read by two kernels as well.)
   bool cluster = false;
   if (slots == 8) {
     int runs = 1;

@@ -8,8 +8,9 @@
 
 namespace msd {
 
-// n / d for 0 <= n < 2^31 and 1 <= d < 2^31 by a multiplication: with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1,
-// n / d = (mulhi(n, m) + n) >> s (the sum stays below 2^32).
+// n / d for 0 <= n < 2^31 and 1 <= d < 2^31 by a multiplication (T. Granlund, P. L. Montgomery, Division by invariant integers using multiplication,
+// PLDI 1994): with s = ceil(log2 d) and m' = 2^32 + m = floor(2^(32 + s) / d) + 1, m' d lies between 2^(32 + s) + 1 and 2^(32 + s) + 2^s, which is near enough for
+// n / d = floor(m' n / 2^(32 + s)) = (mulhi(n, m) + n) >> s (the sum stays below 2^32).
 struct FastDiv {
   uint32_t d, mul, shift;
 };

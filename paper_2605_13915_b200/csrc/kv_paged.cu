@@ -200,8 +200,8 @@ template <bool kInt8, int kVecs>
 msd_status_t launch_append(AppendParams& p, cudaStream_t s) {
   const int64_t per = kAppendThreads / 32, ctas = (p.n_rows * p.head_groups + per - 1) / per, most = 64LL * sm_count();
   p.row_ctas = static_cast<int>(ctas < most ? ctas : most);
-  const int checkers = (p.B + kCheckedBy - 1) / kCheckedBy;
-  return launch_pdl(kv_append_kernel<kInt8, kVecs>, dim3(p.row_ctas + checkers), dim3(kAppendThreads), 0, s, option(OPT_NO_PDL) != 1, p) == cudaSuccess
+  const int check_ctas = (p.B + kCheckedBy - 1) / kCheckedBy;
+  return launch_pdl(kv_append_kernel<kInt8, kVecs>, dim3(p.row_ctas + check_ctas), dim3(kAppendThreads), 0, s, option(OPT_NO_PDL) != 1, p) == cudaSuccess
              ? MSD_OK
              : (cudaGetLastError(), MSD_ERR_CUDA);
 }
